@@ -20,6 +20,7 @@ FAMILY_FDPA, FAMILY_FTZ_ADDMUL, FAMILY_GST_FDPA, FAMILY_FMA = 0, 1, 2, 3
 SCALE_FORMAT_E8M0, SCALE_FORMAT_UE4M3 = 0, 1
 GEN_ZERO, GEN_FINITE_BITS, GEN_UNIFORM_EXP, GEN_RANDOM_BITS, GEN_NORMAL = 0, 1, 2, 3, 4
 GEN_UNIFORM, GEN_NORMAL_OUTLIERS, GEN_CANCELLING, GEN_SIGNED_ZEROS = 5, 6, 7, 8
+SCALE_RULE_FLOOR, SCALE_RULE_FIT = 0, 1
 SCALE_NONE, SCALE_TENSOR, SCALE_TILE, SCALE_FACTOR = 0, 1, 2, 3
 (MFMA_F32_16X16X16_F16, MFMA_F32_16X16X16_BF16, MFMA_F32_32X32X8_F16, MFMA_F32_32X32X8_BF16,
  MFMA_F32_16X16X32_F16, MFMA_F32_16X16X32_BF16, MFMA_F32_16X16X32_FP8_FP8, MFMA_F32_16X16X32_FP8_BF8,
@@ -141,6 +142,9 @@ _lib.mmaemu_exact_dot_sample.argtypes = [_vp, _vp, _vp, _u32, _u32, _u32, Dtypes
 _lib.mmaemu_deviation_hist_reset.argtypes = [_vp, _vp]
 _lib.mmaemu_deviation_sample.argtypes = [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u64, Dtypes, _u64, ctypes.c_int32, _vp, _vp]
 _lib.mmaemu_deviation_sample_kernel.argtypes = [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u64, Dtypes, _u64, ctypes.POINTER(ctypes.c_char_p)]
+_lib.mmaemu_rmsnorm_quantize.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _u64, _u32, _u64, _u64, ctypes.c_int, ctypes.c_int, ctypes.c_int, _u32, ctypes.c_double, _vp]
+_lib.mmaemu_quantize_fp4.argtypes = [_vp, _vp, _vp, _vp, _u64, _u32, _u64, ctypes.c_int, _u32, _u32, ctypes.c_float, _vp]
+_lib.mmaemu_matmul_fp4.argtypes = [_vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u64, _u64, ctypes.c_int, ctypes.c_int, _u32, ctypes.c_float, _vp]
 
 
 def _status_string(s):
@@ -316,6 +320,26 @@ def deviation_sample_kernel(A, B, C, D, m, n, k, batch, dtypes, stride):
     _check(_lib.mmaemu_deviation_sample_kernel(_ptr(A), _ptr(B), _ptr(C) if C is not None else None, _ptr(D), m, n, k, batch, dt, stride,
                                                ctypes.byref(name)))
     return name.value.decode()
+
+
+def rmsnorm_quantize(x, residual, weight, residual_out, codes, scales, rows, cols, type, weight_type, code_type, scale_rule=SCALE_RULE_FLOOR,
+                     eps=1e-6, x_stride=0, residual_stride=0, stream=None):
+    """Norm of x + residual (None: of x) to 8-bit codes with E8M0 scales per 32 elements; rows padded to multiples of 32 in codes and scales."""
+    _check(_lib.mmaemu_rmsnorm_quantize(_ptr(x), _ptr(residual), _ptr(weight), _ptr(residual_out), _ptr(codes), _ptr(scales), rows, cols, x_stride,
+                                        residual_stride, type, weight_type, code_type, scale_rule, eps, _stream(stream)))
+
+
+def quantize_fp4(x, codes, scales, values, rows, cols, type, scale_format=SCALE_FORMAT_E8M0, scale_rule=SCALE_RULE_FLOOR, tensor_scale=1.0, x_stride=0,
+                 stream=None):
+    """FP4 codes (two to a byte) and group scales of x, and the values they stand for unless `values` is None."""
+    _check(_lib.mmaemu_quantize_fp4(_ptr(x), _ptr(codes), _ptr(scales), _ptr(values), rows, cols, x_stride, type, scale_format, scale_rule, tensor_scale,
+                                    _stream(stream)))
+
+
+def matmul_fp4(A, SA, W, SW, D, m, n, k, a_type, d_type, scale_format=SCALE_FORMAT_E8M0, alpha=1.0, a_stride=0, d_stride=0, stream=None):
+    """D = alpha A W^T with packed FP4 weights; SA: the activations' scales (8-bit types) or None."""
+    _check(_lib.mmaemu_matmul_fp4(_ptr(A), _ptr(SA), _ptr(W), _ptr(SW), _ptr(D), m, n, k, a_stride, d_stride, a_type, d_type, scale_format, alpha,
+                                  _stream(stream)))
 
 
 # ---- unpacking of the device-side result structs (host copies; no arithmetic) -----------

@@ -860,4 +860,86 @@ mmaemu_status mmaemu_deviation_sample_kernel(const void *A, const void *B, const
     return MMAEMU_OK;
 }
 
+static bool is_value_type(uint32_t t) { return t == MMAEMU_BF16 || t == MMAEMU_FP16 || t == MMAEMU_FP32; }
+
+mmaemu_status mmaemu_rmsnorm_quantize(const void *x, const void *residual, const void *weight, void *residual_out, void *codes, void *scales,
+                                      uint64_t rows, uint32_t cols, uint64_t x_stride, uint64_t residual_stride, mmaemu_dtype type,
+                                      mmaemu_dtype weight_type, mmaemu_dtype code_type, uint32_t scale_rule, double eps, void *hip_stream)
+{
+    if (!is_value_type(type) || (weight_type != type && weight_type != MMAEMU_FP32)) {
+        set_error("rmsnorm_quantize: type must be BF16, FP16 or FP32, and weight_type the same or FP32");
+        return MMAEMU_ERR_UNSUPPORTED;
+    }
+    if (code_type != MMAEMU_FP8_E4M3 && code_type != MMAEMU_FP8_E5M2) { set_error("rmsnorm_quantize: codes are E4M3 or E5M2"); return MMAEMU_ERR_UNSUPPORTED; }
+    if (scale_rule > MMAEMU_SCALE_RULE_FIT) { set_error("rmsnorm_quantize: scale rule out of range"); return MMAEMU_ERR_INVALID_ARG; }
+    if (!(eps >= 0.0) || eps > 1.7976931348623157e308) { set_error("rmsnorm_quantize: eps must be finite and not negative"); return MMAEMU_ERR_INVALID_ARG; }
+    if (x_stride == 0) x_stride = cols;
+    if (residual_stride == 0) residual_stride = cols;
+    if (cols == 0 || cols > (1u << 24)) { set_error("rmsnorm_quantize: cols=%u outside 1 .. 2^24", cols); return MMAEMU_ERR_SHAPE; }
+    const uint64_t widest = x_stride > residual_stride ? x_stride : residual_stride;
+    if (x_stride < cols || residual_stride < cols || widest >= (1ull << 48) || rows > (1ull << 48) / widest) {
+        set_error("rmsnorm_quantize: a stride below cols, or rows * stride of 2^48 and more");
+        return MMAEMU_ERR_SHAPE;
+    }
+    if (residual_out && !residual) { set_error("rmsnorm_quantize: residual_out needs a residual"); return MMAEMU_ERR_INVALID_ARG; }
+    if (residual_out && residual_out == x && x_stride != residual_stride) { set_error("rmsnorm_quantize: residual_out = x needs equal strides"); return MMAEMU_ERR_INVALID_ARG; }
+    if (rows == 0) return MMAEMU_OK;
+    if (!x || !codes || !scales) { set_error("rmsnorm_quantize: NULL device pointer"); return MMAEMU_ERR_INVALID_ARG; }
+    const uintptr_t mask = type == MMAEMU_FP32 ? 3 : 1, wmask = weight_type == MMAEMU_FP32 ? 3 : 1;
+    if ((((uintptr_t)x | (uintptr_t)residual | (uintptr_t)residual_out) & mask) || ((uintptr_t)weight & wmask)) {
+        set_error("rmsnorm_quantize: pointers must be aligned to their element size");
+        return MMAEMU_ERR_INVALID_ARG;
+    }
+    return launch_rmsnorm_quantize(x, residual, weight, residual_out, codes, scales, rows, cols, x_stride, residual_stride, type, weight_type, code_type,
+                                   scale_rule, eps, (hipStream_t)hip_stream);
+}
+
+mmaemu_status mmaemu_quantize_fp4(const void *x, void *codes, void *scales, void *values, uint64_t rows, uint32_t cols, uint64_t x_stride,
+                                  mmaemu_dtype type, uint32_t scale_format, uint32_t scale_rule, float tensor_scale, void *hip_stream)
+{
+    if (!is_value_type(type)) { set_error("quantize_fp4: type must be BF16, FP16 or FP32"); return MMAEMU_ERR_UNSUPPORTED; }
+    if (scale_format > MMAEMU_SCALE_FORMAT_UE4M3 || scale_rule > MMAEMU_SCALE_RULE_FIT) { set_error("quantize_fp4: scale format or rule out of range"); return MMAEMU_ERR_INVALID_ARG; }
+    if (scale_format == MMAEMU_SCALE_FORMAT_UE4M3 && scale_rule != MMAEMU_SCALE_RULE_FLOOR) { set_error("quantize_fp4: the scale rules belong to E8M0"); return MMAEMU_ERR_INVALID_ARG; }
+    if (!(tensor_scale > 0.0f) || tensor_scale > 3.402823466e38f || (scale_format == MMAEMU_SCALE_FORMAT_E8M0 && tensor_scale != 1.0f)) {
+        set_error("quantize_fp4: tensor_scale must be positive and finite, and 1 with E8M0 scales");
+        return MMAEMU_ERR_INVALID_ARG;
+    }
+    if (x_stride == 0) x_stride = cols;
+    if (cols == 0 || cols > (1u << 24)) { set_error("quantize_fp4: cols=%u outside 1 .. 2^24", cols); return MMAEMU_ERR_SHAPE; }
+    if (x_stride < cols || x_stride >= (1ull << 48) || rows > (1ull << 48) / x_stride) {
+        set_error("quantize_fp4: x_stride below cols, or rows * x_stride of 2^48 and more");
+        return MMAEMU_ERR_SHAPE;
+    }
+    if (values && values == x && x_stride != cols) { set_error("quantize_fp4: values = x needs x_stride = cols"); return MMAEMU_ERR_INVALID_ARG; }
+    if (rows == 0) return MMAEMU_OK;
+    if (!x || !codes || !scales) { set_error("quantize_fp4: NULL device pointer"); return MMAEMU_ERR_INVALID_ARG; }
+    if (((uintptr_t)x | (uintptr_t)values) & (type == MMAEMU_FP32 ? 3 : 1)) { set_error("quantize_fp4: pointers must be aligned to their element size"); return MMAEMU_ERR_INVALID_ARG; }
+    return launch_quantize_fp4(x, codes, scales, values, rows, cols, x_stride, type, scale_format, scale_rule, tensor_scale, (hipStream_t)hip_stream);
+}
+
+mmaemu_status mmaemu_matmul_fp4(const void *A, const void *SA, const void *W, const void *SW, void *D, uint32_t m, uint32_t n, uint32_t k,
+                                uint64_t a_stride, uint64_t d_stride, mmaemu_dtype a_type, mmaemu_dtype d_type, uint32_t scale_format, float alpha,
+                                void *hip_stream)
+{
+    const bool bytes = a_type == MMAEMU_FP8_E4M3 || a_type == MMAEMU_FP8_E5M2;
+    if (!bytes && a_type != MMAEMU_BF16 && a_type != MMAEMU_FP16) { set_error("matmul_fp4: activations are BF16, FP16, E4M3 or E5M2"); return MMAEMU_ERR_UNSUPPORTED; }
+    if (!is_value_type(d_type)) { set_error("matmul_fp4: outputs are FP32, BF16 or FP16"); return MMAEMU_ERR_UNSUPPORTED; }
+    if (scale_format > MMAEMU_SCALE_FORMAT_UE4M3) { set_error("matmul_fp4: scale format out of range"); return MMAEMU_ERR_INVALID_ARG; }
+    if (bytes && scale_format != MMAEMU_SCALE_FORMAT_E8M0) { set_error("matmul_fp4: 8-bit activations go with E8M0 weight scales"); return MMAEMU_ERR_UNSUPPORTED; }
+    if (!(alpha >= -3.402823466e38f && alpha <= 3.402823466e38f)) { set_error("matmul_fp4: alpha must be finite"); return MMAEMU_ERR_INVALID_ARG; }
+    if (n == 0 || k == 0 || k % 32 || k > (1u << 20)) { set_error("matmul_fp4: n=%u k=%u: neither zero, k a multiple of 32 up to 2^20", n, k); return MMAEMU_ERR_SHAPE; }
+    if (m > (1u << 24) || n > (1u << 24)) { set_error("matmul_fp4: m or n above 2^24"); return MMAEMU_ERR_SHAPE; }
+    if (a_stride == 0) a_stride = k;
+    if (d_stride == 0) d_stride = n;
+    if (a_stride < k || d_stride < n || a_stride > (1ull << 38) || d_stride > (1ull << 38)) { set_error("matmul_fp4: a stride below its row's length or above 2^38"); return MMAEMU_ERR_SHAPE; }
+    if (m == 0) return MMAEMU_OK;
+    if (!A || !W || !SW || !D || (bytes && !SA)) { set_error("matmul_fp4: NULL device pointer"); return MMAEMU_ERR_INVALID_ARG; }
+    if (!bytes && SA) { set_error("matmul_fp4: 16-bit activations take no scales"); return MMAEMU_ERR_INVALID_ARG; }
+    if ((((uintptr_t)A | (uintptr_t)W | (uintptr_t)(a_stride * (bytes ? 1 : 2))) & 15) || ((uintptr_t)D & (d_type == MMAEMU_FP32 ? 3 : 1))) {
+        set_error("matmul_fp4: A, its rows and W must be aligned to 16 bytes, D to its element size");
+        return MMAEMU_ERR_INVALID_ARG;
+    }
+    return launch_matmul_fp4(A, SA, W, SW, D, m, n, k, a_stride, d_stride, a_type, d_type, scale_format, alpha, (hipStream_t)hip_stream);
+}
+
 } // extern "C"

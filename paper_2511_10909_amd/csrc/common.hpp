@@ -167,6 +167,15 @@ mmaemu_status launch_deviation_sample(const void *A, const void *B, const uint32
 const char *deviation_kernel_name(const void *A, const void *B, const void *C, const void *D, uint32_t m, uint32_t n, uint32_t k, uint64_t batch,
                                   uint32_t ta, uint32_t tb, uint64_t stride);
 
+// block-scaled operators: norm to 8 bits (rmsnorm.hip), weights to FP4 (quantize_fp4.hip), products with them (matmul_fp4.hip)
+mmaemu_status launch_rmsnorm_quantize(const void *x, const void *residual, const void *weight, void *residual_out, void *codes, void *scales,
+                                      uint64_t rows, uint32_t cols, uint64_t x_stride, uint64_t residual_stride, uint32_t type,
+                                      uint32_t weight_type, uint32_t code_type, uint32_t scale_rule, double eps, hipStream_t s);
+mmaemu_status launch_quantize_fp4(const void *x, void *codes, void *scales, void *values, uint64_t rows, uint32_t cols, uint64_t x_stride,
+                                  uint32_t type, uint32_t scale_format, uint32_t scale_rule, float tensor_scale, hipStream_t s);
+mmaemu_status launch_matmul_fp4(const void *A, const void *SA, const void *W, const void *SW, void *D, uint32_t m, uint32_t n, uint32_t k,
+                                uint64_t a_stride, uint64_t d_stride, uint32_t a_type, uint32_t d_type, uint32_t scale_format, float alpha, hipStream_t s);
+
 // issue-rate probes (issue_rate.hip)
 uint32_t issue_probe_count();
 const char *issue_probe_name(uint32_t op);

@@ -1,0 +1,139 @@
+// Operands of the products with packed FP4 weights: what a lane of the 16 x 16 matrix instructions holds, from memory as it
+// lies.  The weights are the first operand and the activations the second, so that a lane ends with four consecutive
+// outputs of one token.
+//
+// A window is 128 products of a row.  Lane l holds weight row l % 16, codes 32 g .. 32 g + 31 of the window with g = l / 16:
+// sixteen bytes, all under one E8M0 scale or two UE4M3 scales.
+//   8-bit activations, v_mfma_scale_f32_16x16x128_f8f6f4: token l % 16, k = 16 g .. + 15 and 64 + 16 g .. + 15; the scale
+//     operand carries the code of block g in its low byte.
+//   16-bit activations, four v_mfma_f32_16x16x32: the sum does not mind which k an instruction takes, so instruction j takes
+//     k = 32 g + 8 j + i from lane l (i = 0 .. 7): both operands are then contiguous in memory and every lane stays in one block.
+#pragma once
+#include "block_scale.hpp"
+
+namespace mmaemu {
+
+// Weights of 16-bit activations are brought to the activations' type, scale included.  That is exact: E2M1 2^(code - 127) is
+// a BF16 number (from magnitude 2^128 on an infinity, as in binary32), E2M1 UE4M3 has six significant bits and lies in
+// 2^-10 .. 2688, within FP16.  FP16 weights under E8M0 scales are exact for codes 104 .. 140 (2^-23 .. 2^13); other codes
+// take the BF16 way, with the activations split into two BF16 numbers (their eleven bits fit two times eight).
+__device__ __forceinline__ bool fp16_holds(uint32_t code) { return code - 104u <= 36u; }
+
+struct Frag16 { u32x4 w; };                        // eight 16-bit elements
+
+__device__ __forceinline__ Frag16 weights_bf16(uint32_t codes, uint32_t e8m0)
+{
+    const float s = __uint_as_float(e8m0 << 23);   // (field 0 is read as 2^-127, field 255 as NaN)
+    Frag16 f;
+    f.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0));
+    f.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1));
+    f.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2));
+    f.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3));
+    return f;
+}
+__device__ __forceinline__ Frag16 weights_fp16(uint32_t codes, uint32_t e8m0)
+{
+    const float s = __uint_as_float(e8m0 << 23);
+    Frag16 f;
+    f.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 0));
+    f.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 1));
+    f.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 2));
+    f.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 3));
+    return f;
+}
+// under a UE4M3 scale, given in binary32 (BF16) or twice in FP16
+__device__ __forceinline__ Frag16 weights_bf16_by(uint32_t codes, float s)
+{
+    Frag16 f;
+    const f32x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 1),
+                p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 3);
+    f.w[0] = float_elem<MMAEMU_BF16>(p0[0] * s) | float_elem<MMAEMU_BF16>(p0[1] * s) << 16;
+    f.w[1] = float_elem<MMAEMU_BF16>(p1[0] * s) | float_elem<MMAEMU_BF16>(p1[1] * s) << 16;
+    f.w[2] = float_elem<MMAEMU_BF16>(p2[0] * s) | float_elem<MMAEMU_BF16>(p2[1] * s) << 16;
+    f.w[3] = float_elem<MMAEMU_BF16>(p3[0] * s) | float_elem<MMAEMU_BF16>(p3[1] * s) << 16;
+    return f;
+}
+__device__ __forceinline__ Frag16 weights_fp16_by(uint32_t codes, f16x2 s)
+{
+    Frag16 f;
+    f.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 0) * s);
+    f.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 1) * s);
+    f.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 2) * s);
+    f.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 3) * s);
+    return f;
+}
+
+// eight FP16 activations, times 1 or 4, as sums of two BF16 numbers each (the weights of codes 253 and 254 reach 2^128: they are
+// taken at a quarter there, so that no infinity meets a zero of the smaller parts)
+__device__ __forceinline__ void split_fp16(const Frag16 &x, float factor, Frag16 &hi, Frag16 &lo)
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float a = elem_float<MMAEMU_FP16>(x.w[q] & 0xFFFFu) * factor, b = elem_float<MMAEMU_FP16>(x.w[q] >> 16) * factor;
+        const uint32_t ha = float_elem<MMAEMU_BF16>(a), hb = float_elem<MMAEMU_BF16>(b);
+        const float ra = a - __uint_as_float(ha << 16), rb = b - __uint_as_float(hb << 16);
+        hi.w[q] = ha | hb << 16;
+        // (an infinity leaves no remainder: infinity minus itself is NaN)
+        lo.w[q] = (magnitude(a) >= 0x7F800000u ? 0u : float_elem<MMAEMU_BF16>(ra)) | (magnitude(b) >= 0x7F800000u ? 0u : float_elem<MMAEMU_BF16>(rb)) << 16;
+    }
+}
+
+__device__ __forceinline__ f32x4 mfma_bf16(const Frag16 &a, const Frag16 &b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.w), __builtin_bit_cast(bf16x8, b.w), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma_fp16(const Frag16 &a, const Frag16 &b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.w), __builtin_bit_cast(f16x8, b.w), c, 0, 0, 0);
+}
+// AT: MMAEMU_FP8_E4M3 or MMAEMU_FP8_E5M2 (formats 0 and 1 of the instruction; 4 is E2M1)
+template <int AT> __device__ __forceinline__ f32x4 mfma_scaled(u32x4 w, uint32_t sw, const i32x8 &x, uint32_t sx, f32x4 c)
+{
+    const i32x8 a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, x, c, 4, AT == MMAEMU_FP8_E5M2 ? 1 : 0, 0, (int)sw, 0, (int)sx);
+}
+
+struct ProductArgs {
+    const uint8_t *A, *SA, *W, *SW;
+    void *D;
+    uint64_t a_stride, d_stride;                   // of A in bytes, of D in elements
+    uint32_t m, n, k;
+    uint32_t d_type;
+    float alpha;
+};
+
+// four consecutive outputs of one token, columns j .. j + 3
+__device__ __forceinline__ void store_outputs(const ProductArgs &p, uint32_t i, uint32_t j, f32x4 v)
+{
+    if (i >= p.m || j >= p.n) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] *= p.alpha;
+    const uint64_t at = (uint64_t)i * p.d_stride + j;
+    const int left = p.n - j < 4u ? (int)(p.n - j) : 4;
+    if (p.d_type == MMAEMU_FP32) {
+        float *d = (float *)p.D + at;
+        if (left == 4) {
+            Words4<4> o;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o.w[q] = __float_as_uint(v[q]);
+            *reinterpret_cast<Words4<4> *>(d) = o;
+        } else
+            for (int q = 0; q < left; ++q) d[q] = v[q];
+        return;
+    }
+    uint32_t e[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) e[q] = p.d_type == MMAEMU_BF16 ? float_elem<MMAEMU_BF16>(v[q]) : float_elem<MMAEMU_FP16>(v[q]);
+    uint16_t *d = (uint16_t *)p.D + at;
+    if (left == 4) {
+        Words2<2> o;
+        o.w[0] = e[0] | e[1] << 16;
+        o.w[1] = e[2] | e[3] << 16;
+        *reinterpret_cast<Words2<2> *>(d) = o;
+    } else
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+            if (q < left) d[q] = (uint16_t)e[q];
+}
+
+} // namespace mmaemu

@@ -1,0 +1,414 @@
+"""The block-scaled operators on the GPU against the binary64 oracle: norm to 8 bits, weights to FP4, products with FP4 weights."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_scale as bs
+from paper_2511_10909_amd import binding as mm
+
+pytestmark = pytest.mark.gpu
+NP = {mm.BF16: np.uint16, mm.FP16: np.uint16, mm.FP32: np.uint32}
+GUARD = 0xA5
+
+
+def dev(a):
+    """A numpy array of bit patterns on the GPU, as bytes."""
+    return torch.from_numpy(np.ascontiguousarray(a).view(np.uint8).reshape(-1).copy()).cuda()
+
+
+def host(t, dtype, shape):
+    return t.cpu().numpy().view(dtype).reshape(shape)
+
+
+def rows_of(rng, rows, cols, t, spread=3):
+    return bs.bits_of((rng.standard_normal((rows, cols)) * np.exp2(rng.integers(-spread, spread + 1, (rows, cols)))).astype(np.float32), t)
+
+
+def strided(a, stride):
+    wide = np.full((a.shape[0], stride), 0x55, dtype=a.dtype)
+    wide[:, :a.shape[1]] = a
+    return wide
+
+
+# ---- norm -----------------------------------------------------------------------------------
+
+def run_norm(x, residual, weight, t, wt, code, rule, eps, xs=0, rs=0, place="own", stream=None):
+    """(codes, scales, residual stream) as numpy arrays; guards behind the outputs stay as they were."""
+    rows, cols = x.shape
+    k = -(-cols // 32) * 32
+    xs, rs = xs or cols, rs or cols
+    dx = dev(strided(x, xs))
+    dr = None if residual is None else dev(strided(residual, rs))
+    dw = None if weight is None else dev(weight)
+    es = x.dtype.itemsize
+    out = None
+    if residual is not None:
+        out = {"own": torch.full((rows * rs * es + 64,), GUARD, dtype=torch.uint8, device="cuda"), "residual": dr, "x": dx, "none": None}[place]
+    codes = torch.full((rows * k + 64,), GUARD, dtype=torch.uint8, device="cuda")
+    scales = torch.full((rows * k // 32 + 64,), GUARD, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    mm.rmsnorm_quantize(dx, dr, dw, out, codes, scales, rows, cols, t, wt, code, rule, eps, xs, rs, stream=stream)
+    torch.cuda.synchronize()
+    c, s = codes.cpu().numpy(), scales.cpu().numpy()
+    assert (c[rows * k:] == GUARD).all() and (s[rows * k // 32:] == GUARD).all()
+    h = None
+    if out is not None:
+        raw = out.cpu().numpy()
+        if place == "own":
+            assert (raw[rows * rs * es:] == GUARD).all()
+        h = raw[:rows * rs * es].view(x.dtype).reshape(rows, rs)
+        rest = h[:, cols:]
+        assert (rest == (np.frombuffer(bytes([GUARD]) * es, dtype=x.dtype)[0] if place == "own" else 0x55)).all()
+        h = h[:, :cols]
+    return c[:rows * k].reshape(rows, k), s[:rows * k // 32].reshape(rows, k // 32), h
+
+
+def check_norm(x, residual, weight, t, wt, code, rule, eps, **kw):
+    wv = None if weight is None else bs.values_of(weight, wt)
+    h, y = bs.rmsnorm(x, residual, wv, t, eps)
+    wc, ws = bs.quantize8(y, code, rule)
+    c, s, gh = run_norm(x, residual, weight, t, wt, code, rule, eps, **kw)
+    # y is rounded once from binary64, in which both sides agree to parts in 2^50: the codes are equal
+    assert np.array_equal(s, ws)
+    assert np.array_equal(c, wc)
+    if gh is not None:
+        same = (gh == h) | (np.isnan(bs.values_of(gh, t)) & np.isnan(bs.values_of(h, t)))
+        assert same.all()
+
+
+@pytest.mark.parametrize("cols", [1, 2, 31, 32, 33, 100, 512, 513, 2048, 2100, 4096, 5000, 8192, 8200, 16384, 20000, 32768, 32801, 70000])
+@pytest.mark.parametrize("t", [mm.BF16, mm.FP16, mm.FP32])
+def test_norm_lengths(cols, t):
+    rng = np.random.default_rng(cols)
+    rows = 5 if cols < 10000 else 2
+    x, r = rows_of(rng, rows, cols, t), rows_of(rng, rows, cols, t)
+    w = rows_of(rng, 1, cols, t, 0)[0]
+    check_norm(x, r, w, t, t, mm.E4M3, bs.FLOOR, 1e-6)
+    check_norm(x, None, None, t, t, mm.E5M2, bs.FIT, 1e-5)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 63, 257])
+@pytest.mark.parametrize("code,rule", [(mm.E4M3, bs.FLOOR), (mm.E4M3, bs.FIT), (mm.E5M2, bs.FLOOR), (mm.E5M2, bs.FIT)])
+def test_norm_rows_strides_and_weights(rows, code, rule):
+    rng = np.random.default_rng(rows)
+    for t, wt, cols, xs, rs in ((mm.BF16, mm.FP32, 357, 359, 400), (mm.FP16, mm.FP16, 1028, 1028, 1031), (mm.FP32, mm.FP32, 96, 97, 0)):
+        x, r, w = rows_of(rng, rows, cols, t), rows_of(rng, rows, cols, t), rows_of(rng, 1, cols, wt, 0)[0]
+        check_norm(x, r, w, t, wt, code, rule, 1e-6, xs=xs, rs=rs)
+        check_norm(x, r, w, t, wt, code, rule, 1e-6, xs=xs, rs=rs, place="none")
+
+
+@pytest.mark.parametrize("cols", [40, 4096, 33000])
+def test_norm_residual_in_place(cols):
+    rng = np.random.default_rng(cols)
+    x, r = rows_of(rng, 3, cols, mm.BF16), rows_of(rng, 3, cols, mm.BF16)
+    for place in ("residual", "x"):
+        check_norm(x, r, None, mm.BF16, mm.BF16, mm.E4M3, bs.FLOOR, 1e-6, xs=cols + 3, rs=cols + 3, place=place)
+
+
+@pytest.mark.parametrize("cols", [64, 4096, 40000])
+def test_norm_of_rows_without_ordinary_numbers(cols):
+    """Rows of zeros (eps and no eps), an infinity, a NaN, binary32 rows whose squares leave binary32 on either side, subnormal ones."""
+    rng = np.random.default_rng(7)
+    v = rng.standard_normal((8, cols)).astype(np.float32)
+    v[1] = 0
+    v[2, cols // 2] = np.inf
+    v[3, 5] = np.nan
+    v[4] *= np.float32(1e30)
+    v[5] *= np.float32(1e-30)
+    v[6] *= np.float32(1e-41)
+    v[7, :32] = 0
+    for eps in (1e-6, 0.0):
+        check_norm(v.view(np.uint32), None, None, mm.FP32, mm.FP32, mm.E4M3, bs.FLOOR, eps)
+        check_norm(bs.bits_of(v, mm.BF16), None, None, mm.BF16, mm.BF16, mm.E5M2, bs.FIT, eps)
+    w = np.ones(cols, dtype=np.float32)
+    w[0], w[40], w[41] = np.inf, np.nan, 3e38                          # weights that no number holds
+    check_norm(v.view(np.uint32), None, w.view(np.uint32), mm.FP32, mm.FP32, mm.E4M3, bs.FIT, 1e-6)
+
+
+def test_norm_at_the_scale_rules_borders():
+    """Rows that make y a power of two, the largest code, and just beyond: mean square 1, eps 0, weights carry the values."""
+    cols = 128
+    x = np.where(np.arange(cols) % 2, -1.0, 1.0).astype(np.float32)[None]
+    for vals in ((448.0, 447.999, 448.001, 449.0), (256.0, 255.9999, 512.0, 464.0), (2.0 ** -130, 2.0 ** -126, 2.0 ** -149, 3.0), (57344.0, 57345.0, 2.0 ** 127, 65536.0)):
+        w = np.zeros(cols, dtype=np.float32)
+        w[0], w[33], w[66], w[99] = vals
+        w[1::32] = np.float32(17.0 / 16)
+        for code in (mm.E4M3, mm.E5M2):
+            for rule in (bs.FLOOR, bs.FIT):
+                check_norm(x.view(np.uint32), None, w.view(np.uint32), mm.FP32, mm.FP32, code, rule, 0.0)
+
+
+# ---- weights to FP4 ---------------------------------------------------------------------------
+
+def run_quantize(x, t, fmt, rule, ts, xs=0, want_values=True):
+    rows, cols = x.shape
+    k = -(-cols // 32) * 32
+    b = 32 if fmt == bs.SCALE_E8M0 else 16
+    dx = dev(strided(x, xs or cols))
+    codes = torch.full((rows * k // 2 + 64,), GUARD, dtype=torch.uint8, device="cuda")
+    scales = torch.full((rows * k // b + 64,), GUARD, dtype=torch.uint8, device="cuda")
+    es = x.dtype.itemsize
+    values = torch.full((rows * cols * es + 64,), GUARD, dtype=torch.uint8, device="cuda") if want_values else None
+    mm.quantize_fp4(dx, codes, scales, values, rows, cols, t, fmt, rule, ts, xs)
+    torch.cuda.synchronize()
+    c, s = codes.cpu().numpy(), scales.cpu().numpy()
+    assert (c[rows * k // 2:] == GUARD).all() and (s[rows * k // b:] == GUARD).all()
+    v = None
+    if want_values:
+        raw = values.cpu().numpy()
+        assert (raw[rows * cols * es:] == GUARD).all()
+        v = raw[:rows * cols * es].view(x.dtype).reshape(rows, cols)
+    return c[:rows * k // 2].reshape(rows, -1), s[:rows * k // b].reshape(rows, -1), v
+
+
+def check_quantize(x, t, fmt, rule=bs.FLOOR, ts=1.0, **kw):
+    wc, ws, wv = bs.quantize_fp4(bs.values_of(x, t), fmt, rule, ts)
+    c, s, v = run_quantize(x, t, fmt, rule, ts, **kw)
+    assert np.array_equal(s, ws)
+    assert np.array_equal(c, wc)
+    if v is not None:
+        got = bs.values_of(v, t)
+        assert np.array_equal(np.isnan(got), np.isnan(wv))
+        ok = ~np.isnan(wv)
+        # one rounding of the exact value: half a step, and half the least subnormal
+        step = {mm.BF16: 2.0 ** -9, mm.FP16: 2.0 ** -12, mm.FP32: 2.0 ** -25}[t] * 2
+        least = {mm.BF16: 2.0 ** -134, mm.FP16: 2.0 ** -25, mm.FP32: 2.0 ** -150}[t]
+        big = {mm.BF16: 3.3895313892515355e38, mm.FP16: 65504.0, mm.FP32: 3.4028234663852886e38}[t]
+        inside = ok & (np.abs(wv) <= big)
+        assert (np.abs(got[inside] - wv[inside]) <= np.maximum(np.abs(wv[inside]) * step, least)).all()
+        if t != mm.FP16 and fmt == bs.SCALE_E8M0:
+            assert np.array_equal(got[inside], wv[inside])             # two bits and a power of two: exact
+
+
+@pytest.mark.parametrize("rows,cols,xs", [(1, 1, 0), (3, 31, 0), (2, 33, 0), (7, 64, 0), (5, 100, 103), (64, 512, 0), (33, 1000, 1001), (3, 4096, 0), (129, 40, 0), (1, 70001, 0)])
+@pytest.mark.parametrize("t", [mm.BF16, mm.FP16, mm.FP32])
+def test_quantize_shapes(rows, cols, xs, t):
+    x = rows_of(np.random.default_rng(rows * cols), rows, cols, t, 4)
+    check_quantize(x, t, bs.SCALE_E8M0, bs.FLOOR, xs=xs)
+    check_quantize(x, t, bs.SCALE_E8M0, bs.FIT, xs=xs, want_values=False)
+    check_quantize(x, t, bs.SCALE_UE4M3, ts=float(np.float32(0.0123)), xs=xs)
+    check_quantize(x, t, bs.SCALE_UE4M3, ts=0.5, xs=xs)
+
+
+@pytest.mark.parametrize("fmt", [bs.SCALE_E8M0, bs.SCALE_UE4M3])
+def test_quantize_ties_extremes_and_groups_without_numbers(fmt):
+    rng = np.random.default_rng(3)
+    ties = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0])
+    x = np.zeros((40, 64), dtype=np.float32)
+    for i in range(16):                                                # ties at every scale significand
+        s = (8 + i % 8) / 8 * 2.0 ** (i - 8)
+        x[i, :] = rng.choice(np.concatenate([ties, -ties]), 64) * s
+        x[i, 0] = x[i, 16] = x[i, 32] = x[i, 48] = 6 * s
+    x[16, :] = -0.0
+    x[17, 3] = np.nan
+    x[18, 20] = np.inf
+    x[19] = rng.standard_normal(64) * 1e38
+    x[20] = rng.standard_normal(64) * 1e-38
+    x[21] = rng.standard_normal(64) * 1e-44
+    x[22] = np.float32(3.4e38)
+    x[23] = rng.standard_normal(64) * np.exp2(rng.integers(-140, 120, 64).astype(np.float64))
+    x[24:] = rng.standard_normal((16, 64)) * np.exp2(rng.integers(-12, 12, (16, 1)).astype(np.float64))
+    for ts in ((1.0,) if fmt == bs.SCALE_E8M0 else (1.0, 2.0 ** -20, float(np.float32(3.1e-5)), 1e30)):
+        check_quantize(x.view(np.uint32), mm.FP32, fmt, ts=float(np.float32(ts)))
+        check_quantize(bs.bits_of(x, mm.BF16), mm.BF16, fmt, ts=float(np.float32(ts)))
+    if fmt == bs.SCALE_E8M0:
+        check_quantize(x.view(np.uint32), mm.FP32, fmt, bs.FIT)
+
+
+def test_quantize_values_in_place():
+    x = rows_of(np.random.default_rng(1), 37, 200, mm.BF16)
+    _, _, wv = bs.quantize_fp4(bs.values_of(x, mm.BF16), bs.SCALE_E8M0, bs.FIT, 1.0)
+    dx = dev(x)
+    codes = torch.empty(37 * 112, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(37 * 7, dtype=torch.uint8, device="cuda")
+    mm.quantize_fp4(dx, codes, scales, dx, 37, 200, mm.BF16, mm.SCALE_FORMAT_E8M0, mm.SCALE_RULE_FIT)
+    assert np.array_equal(bs.values_of(host(dx, np.uint16, (37, 200)), mm.BF16), wv)
+
+
+# ---- products -----------------------------------------------------------------------------------
+
+def product_bound(a, w, at):
+    """Largest error of a sum of products as the matrix instructions and the additions of partial sums form it.
+
+    16-bit operands (groups of 8, 24 bits): a group's terms are cut at 2^-24 of its largest, the running sum is rounded
+    at 2^-23 or finer in every group; partial sums of at most 32 parts are added.  8-bit operands (groups of 16 in halves of
+    8): the terms of a half are cut at 2^-13 of its largest product (the exponent of a product of significands below 4 may
+    be one below the product's own)."""
+    p = np.abs(a[:, None, :] * w[None, :, :])
+    total = p.sum(-1)
+    k = p.shape[-1]
+    step = 8 if at in (mm.BF16, mm.FP16) else 16
+    chain = (k / step + 40) * 2.0 ** -23 * total
+    halves = p.reshape(p.shape[0], p.shape[1], -1, 8).max(-1).sum(-1)
+    return chain + 8 * (2.0 ** -23 if step == 8 else 2.0 ** -13) * halves
+
+
+def make_operands(rng, m, n, k, at, fmt, lo=118, hi=130):
+    b = 32 if fmt == bs.SCALE_E8M0 else 16
+    W = rng.integers(0, 256, (n, k // 2), dtype=np.uint8)
+    SW = rng.integers(lo, hi, (n, k // b), dtype=np.uint8) if fmt == bs.SCALE_E8M0 else rng.integers(0, 0x7F, (n, k // b), dtype=np.uint8)
+    if at in (mm.BF16, mm.FP16):
+        A, SA = rows_of(rng, m, k, at, 3), None
+        av = bs.values_of(A, at)
+    else:
+        A, SA = bs.quantize8(rng.standard_normal((m, k)) * np.exp2(rng.integers(-2, 3, (m, 1))), at, bs.FLOOR)
+        av = bs.values_of(A, at) * np.repeat(np.exp2(SA.astype(np.float64) - 127), 32, axis=1)
+    return A, SA, W, SW, av, bs.weights(W, SW, fmt)
+
+
+def run_product(A, SA, W, SW, n, at, dt, fmt, alpha=1.0, a_stride=0, d_stride=0, stream=None):
+    m, k = A.shape
+    ds = d_stride or n
+    es = 4 if dt == mm.FP32 else 2
+    dA = dev(strided(A, a_stride or k))
+    D = torch.full((m * ds * es + 64,), GUARD, dtype=torch.uint8, device="cuda")
+    ops = (None if SA is None else dev(SA)), dev(W), dev(SW)
+    torch.cuda.synchronize()
+    mm.matmul_fp4(dA, *ops, D, m, n, k, at, dt, fmt, alpha, a_stride, d_stride, stream=stream)
+    torch.cuda.synchronize()
+    raw = D.cpu().numpy()
+    assert (raw[m * ds * es:] == GUARD).all()
+    full = raw[:m * ds * es].view(NP[dt]).reshape(m, ds)
+    assert (full[:, n:].reshape(-1).view(np.uint8) == GUARD).all()
+    return full[:, :n]
+
+
+def check_product(A, SA, W, SW, av, wv, at, dt, fmt, alpha=1.0, **kw):
+    got = bs.values_of(run_product(A, SA, W, SW, wv.shape[0], at, dt, fmt, alpha, **kw), dt)
+    want = alpha * (av @ wv.T)
+    bound = abs(alpha) * product_bound(av, wv, at)
+    step, least = {mm.BF16: (2.0 ** -8, 2.0 ** -134), mm.FP16: (2.0 ** -11, 2.0 ** -25), mm.FP32: (2.0 ** -23, 2.0 ** -149)}[dt]
+    tol = bound + (np.abs(want) + bound) * step + least
+    big = 65504.0 if dt == mm.FP16 else np.inf
+    # (a product or a partial sum of 2^128 and more is an infinity to the instructions: such outputs are not compared)
+    inside = (np.abs(want) + tol < big) & (np.abs(av) @ np.abs(wv).T < 2.0 ** 127)
+    assert inside.any()
+    assert (np.abs(got - want)[inside] <= tol[inside]).all(), float((np.abs(got - want)[inside] / tol[inside]).max())
+    return got
+
+
+AT_FMT = [(mm.BF16, bs.SCALE_E8M0), (mm.FP16, bs.SCALE_E8M0), (mm.BF16, bs.SCALE_UE4M3), (mm.FP16, bs.SCALE_UE4M3), (mm.E4M3, bs.SCALE_E8M0), (mm.E5M2, bs.SCALE_E8M0)]
+
+
+@pytest.mark.parametrize("at,fmt", AT_FMT)
+@pytest.mark.parametrize("m,n,k", [(1, 1, 32), (1, 16, 128), (1, 33, 96), (2, 17, 160), (3, 100, 1024), (16, 64, 256), (17, 48, 2080), (5, 130, 4128), (40, 65, 544), (64, 64, 512)])
+def test_product_shapes(m, n, k, at, fmt):
+    rng = np.random.default_rng(m * n + k)
+    ops = make_operands(rng, m, n, k, at, fmt)
+    for dt in (mm.FP32, mm.BF16, mm.FP16):
+        check_product(*ops, at, dt, fmt, alpha=0.0625)
+
+
+@pytest.mark.parametrize("at,fmt", AT_FMT)
+def test_product_strides_and_alpha(at, fmt):
+    rng = np.random.default_rng(11)
+    for m, n, k, sa, sd in ((3, 37, 192, 208, 41), (20, 64, 96, 96, 64), (1, 5, 32, 64, 9)):
+        ops = make_operands(rng, m, n, k, at, fmt)
+        check_product(*ops, at, mm.BF16, fmt, alpha=-0.37109375, a_stride=sa, d_stride=sd)
+        check_product(*ops, at, mm.FP32, fmt, alpha=3.0e-5, a_stride=sa, d_stride=sd)
+        got = run_product(*ops[:4], n, at, mm.FP32, fmt, alpha=0.0, a_stride=sa, d_stride=sd)
+        assert not bs.values_of(got, mm.FP32).any()
+
+
+@pytest.mark.parametrize("at", [mm.BF16, mm.FP16])
+def test_product_weights_of_every_scale(at):
+    """E8M0 codes over their whole range with 16-bit activations: FP16 activations leave FP16 weights at codes below 104 and above 140."""
+    rng = np.random.default_rng(5)
+    k = 256
+    for lo, hi in ((0, 4), (96, 112), (136, 148), (0, 120), (100, 200), (228, 242), (236, 247)):
+        ops = make_operands(rng, 4, 48, k, at, bs.SCALE_E8M0, lo, hi)
+        check_product(*ops, at, mm.FP32, bs.SCALE_E8M0, alpha=2.0 ** -14 if lo > 200 else 1.0)
+    A, _, W, SW, _, _ = make_operands(rng, 2, 16, 64, at, bs.SCALE_E8M0)
+    A[:] = bs.bits_of(np.full(A.shape, 2.0 ** -10, dtype=np.float32), at)
+    W[:] = 0x22                                                        # ones
+    SW[:, 0], SW[:, 1] = 254, 127
+    got = bs.values_of(run_product(A, None, W, SW, 16, at, mm.FP32, bs.SCALE_E8M0), mm.FP32)
+    assert (got == 32 * 2.0 ** 117).all()                              # a weight of 2^127 is still a number
+
+
+@pytest.mark.parametrize("at,fmt", AT_FMT)
+def test_product_nan_scales_and_infinities(at, fmt):
+    """A NaN scale of a weight row makes that column NaN, one of an activation row that row; everything else is untouched."""
+    rng = np.random.default_rng(9)
+    m, n, k = 18, 35, 288
+    A, SA, W, SW, av, wv = make_operands(rng, m, n, k, at, fmt)
+    SW[7, 1] = 0xFF
+    SW[34, -1] = 0xFF if fmt == bs.SCALE_E8M0 else 0x7F
+    nan = np.zeros((m, n), dtype=bool)
+    nan[:, [7, 34]] = True
+    if SA is not None:
+        SA[17, 0] = 0xFF
+        nan[17] = True
+    else:
+        A[17, 100] = bs.bits_of(np.float32(np.nan), at)
+        nan[17] = True
+        A[3, 64] = bs.bits_of(np.float32(np.inf), at)
+    got = bs.values_of(run_product(A, SA, W, SW, n, at, mm.FP32, fmt), mm.FP32)
+    if SA is None:
+        w = wv[:, 64]
+        inf = ~nan[3]
+        assert (np.isnan(got[3][inf & (w == 0)])).all() and (got[3][inf & (w > 0)] == np.inf).all() and (got[3][inf & (w < 0)] == -np.inf).all()
+        keep = np.ones(m, dtype=bool)
+        keep[3] = False
+    else:
+        keep = np.ones(m, dtype=bool)
+    assert np.array_equal(np.isnan(got[keep]), nan[keep])
+    fin = ~nan
+    fin[~keep] = False
+    want = np.where(np.isnan(av), 0, av) @ np.where(np.isnan(wv), 0, wv).T
+    assert (np.abs(got - want)[fin] <= (product_bound(np.nan_to_num(av, posinf=0), np.nan_to_num(wv), at) + np.abs(want) * 2.0 ** -23)[fin]).all()
+
+
+def test_product_does_not_depend_on_other_rows():
+    """A row's result is the same alone and among others of its tile where the kernel is the same, and within the bound else."""
+    rng = np.random.default_rng(2)
+    A, SA, W, SW, av, wv = make_operands(rng, 16, 64, 512, mm.BF16, bs.SCALE_E8M0)
+    full = run_product(A, None, W, SW, 64, mm.BF16, mm.FP32, bs.SCALE_E8M0)
+    again = run_product(A, None, W, SW, 64, mm.BF16, mm.FP32, bs.SCALE_E8M0)
+    assert np.array_equal(full, again)
+    one = run_product(A[3:4], None, W, SW, 64, mm.BF16, mm.FP32, bs.SCALE_E8M0)
+    assert (np.abs(bs.values_of(one, mm.FP32) - bs.values_of(full[3:4], mm.FP32)) <= 2 * product_bound(av[3:4], wv, mm.BF16)).all()
+
+
+# ---- together, on another stream, in a graph ----------------------------------------------------
+
+def test_chain_on_a_stream_and_in_a_graph():
+    """Norm, weights and product one after the other on a side stream, captured, and replayed on new inputs."""
+    rng = np.random.default_rng(4)
+    m, n, k = 6, 96, 320
+    w = rows_of(rng, n, k, mm.BF16, 1)
+    side = torch.cuda.Stream()
+    dw, dx = dev(w), torch.zeros(m * k * 2, dtype=torch.uint8, device="cuda")
+    res = torch.zeros(m * k * 2, dtype=torch.uint8, device="cuda")
+    wc, ws = torch.empty(n * k // 2, dtype=torch.uint8, device="cuda"), torch.empty(n * k // 32, dtype=torch.uint8, device="cuda")
+    c, s = torch.empty(m * k, dtype=torch.uint8, device="cuda"), torch.empty(m * k // 32, dtype=torch.uint8, device="cuda")
+    D = torch.empty(m * n * 4, dtype=torch.uint8, device="cuda")
+
+    def work():
+        mm.quantize_fp4(dw, wc, ws, None, n, k, mm.BF16, mm.SCALE_FORMAT_E8M0, mm.SCALE_RULE_FIT)
+        mm.rmsnorm_quantize(dx, res, None, res, c, s, m, k, mm.BF16, mm.BF16, mm.E4M3)
+        mm.matmul_fp4(c, s, wc, ws, D, m, n, k, mm.E4M3, mm.FP32)
+
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        work()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            work()
+    pc, ps, _ = bs.quantize_fp4(bs.values_of(w, mm.BF16), bs.SCALE_E8M0, bs.FIT, 1.0)
+    wv = bs.weights(pc, ps, bs.SCALE_E8M0)
+    for rep in range(3):
+        x, r = rows_of(rng, m, k, mm.BF16), rows_of(rng, m, k, mm.BF16)
+        dx.copy_(dev(x))
+        res.copy_(dev(r))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        h, y = bs.rmsnorm(x, r, None, mm.BF16, 1e-6)
+        qc, qs = bs.quantize8(y, mm.E4M3, bs.FLOOR)
+        assert np.array_equal(host(c, np.uint8, (m, k)), qc) and np.array_equal(host(s, np.uint8, (m, k // 32)), qs)
+        assert np.array_equal(host(res, np.uint16, (m, k)), h)
+        av = bs.values_of(qc, mm.E4M3) * np.repeat(np.exp2(qs.astype(np.float64) - 127), 32, axis=1)
+        got = bs.values_of(host(D, np.uint32, (m, n)), mm.FP32)
+        assert (np.abs(got - av @ wv.T) <= product_bound(av, wv, mm.E4M3) + np.abs(av @ wv.T) * 2.0 ** -23).all()

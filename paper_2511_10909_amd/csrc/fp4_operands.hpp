@@ -10,6 +10,7 @@
 //     k = 32 g + 8 j + i from lane l (i = 0 .. 7): both operands are then contiguous in memory and every lane stays in one block.
 #pragma once
 #include "block_scale.hpp"
+#include <type_traits>
 
 namespace mmaemu {
 
@@ -102,38 +103,49 @@ struct ProductArgs {
     float alpha;
 };
 
-// four consecutive outputs of one token, columns j .. j + 3
-__device__ __forceinline__ void store_outputs(const ProductArgs &p, uint32_t i, uint32_t j, f32x4 v)
+// the kernel for many rows of A (matmul_fp4_tiled.hip)
+mmaemu_status launch_tiled(const ProductArgs &p, uint32_t a_type, uint32_t scale_format, hipStream_t s);
+
+// four consecutive outputs of one token, columns j .. j + 3, in type DT
+template <int DT> __device__ __forceinline__ void store_outputs(const ProductArgs &p, uint32_t i, uint32_t j, f32x4 v)
 {
     if (i >= p.m || j >= p.n) return;
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] *= p.alpha;
     const uint64_t at = (uint64_t)i * p.d_stride + j;
-    const int left = p.n - j < 4u ? (int)(p.n - j) : 4;
-    if (p.d_type == MMAEMU_FP32) {
+    const uint32_t left = p.n - j;
+    if constexpr (DT == MMAEMU_FP32) {
         float *d = (float *)p.D + at;
-        if (left == 4) {
+        if (left >= 4) {
             Words4<4> o;
 #pragma unroll
             for (int q = 0; q < 4; ++q) o.w[q] = __float_as_uint(v[q]);
             *reinterpret_cast<Words4<4> *>(d) = o;
-        } else
-            for (int q = 0; q < left; ++q) d[q] = v[q];
-        return;
+        } else {
+            d[0] = v[0];
+            if (left > 1) d[1] = v[1];
+            if (left > 2) d[2] = v[2];
+        }
+    } else {
+        uint16_t *d = (uint16_t *)p.D + at;
+        if (left >= 4) {
+            Words2<2> o;
+            o.w[0] = float_elem<DT>(v[0]) | float_elem<DT>(v[1]) << 16;
+            o.w[1] = float_elem<DT>(v[2]) | float_elem<DT>(v[3]) << 16;
+            *reinterpret_cast<Words2<2> *>(d) = o;
+        } else {
+            d[0] = (uint16_t)float_elem<DT>(v[0]);
+            if (left > 1) d[1] = (uint16_t)float_elem<DT>(v[1]);
+            if (left > 2) d[2] = (uint16_t)float_elem<DT>(v[2]);
+        }
     }
-    uint32_t e[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) e[q] = p.d_type == MMAEMU_BF16 ? float_elem<MMAEMU_BF16>(v[q]) : float_elem<MMAEMU_FP16>(v[q]);
-    uint16_t *d = (uint16_t *)p.D + at;
-    if (left == 4) {
-        Words2<2> o;
-        o.w[0] = e[0] | e[1] << 16;
-        o.w[1] = e[2] | e[3] << 16;
-        *reinterpret_cast<Words2<2> *>(d) = o;
-    } else
-#pragma unroll
-        for (int q = 0; q < 3; ++q)
-            if (q < left) d[q] = (uint16_t)e[q];
+}
+// f<DT>() for the output type of a launch
+template <class F> __device__ __forceinline__ void with_output_type(uint32_t d_type, F f)
+{
+    if (d_type == MMAEMU_BF16) f(std::integral_constant<int, MMAEMU_BF16>());
+    else if (d_type == MMAEMU_FP16) f(std::integral_constant<int, MMAEMU_FP16>());
+    else f(std::integral_constant<int, MMAEMU_FP32>());
 }
 
 } // namespace mmaemu

@@ -86,7 +86,7 @@ template <int AT, int SF> __global__ void __launch_bounds__(64 * STREAM_WAVES) s
     if (wave) return;
 #pragma unroll
     for (int w = 1; w < STREAM_WAVES; ++w) acc += part[w][lane];
-    store_outputs(p, m0 + (lane & 15u), n0 + 4 * g, acc);
+    with_output_type(p.d_type, [&](auto dt) { store_outputs<dt.value>(p, m0 + (lane & 15u), n0 + 4 * g, acc); });
 }
 
 template <int AT, int SF> static mmaemu_status launch_product(const ProductArgs &p, hipStream_t s)
@@ -102,6 +102,7 @@ mmaemu_status launch_matmul_fp4(const void *A, const void *SA, const void *W, co
     const bool bytes = a_type == MMAEMU_FP8_E4M3 || a_type == MMAEMU_FP8_E5M2;
     const ProductArgs p = {(const uint8_t *)A, (const uint8_t *)SA, (const uint8_t *)W, (const uint8_t *)SW, D, a_stride * (bytes ? 1 : 2), d_stride, m, n, k,
                            d_type, alpha};
+    if (m >= 256) return launch_tiled(p, a_type, scale_format, s);
     if (a_type == MMAEMU_FP8_E4M3) return launch_product<MMAEMU_FP8_E4M3, MMAEMU_SCALE_FORMAT_E8M0>(p, s);
     if (a_type == MMAEMU_FP8_E5M2) return launch_product<MMAEMU_FP8_E5M2, MMAEMU_SCALE_FORMAT_E8M0>(p, s);
     if (scale_format == MMAEMU_SCALE_FORMAT_E8M0)

@@ -291,7 +291,8 @@ AT_FMT = [(mm.BF16, bs.SCALE_E8M0), (mm.FP16, bs.SCALE_E8M0), (mm.BF16, bs.SCALE
 
 
 @pytest.mark.parametrize("at,fmt", AT_FMT)
-@pytest.mark.parametrize("m,n,k", [(1, 1, 32), (1, 16, 128), (1, 33, 96), (2, 17, 160), (3, 100, 1024), (16, 64, 256), (17, 48, 2080), (5, 130, 4128), (40, 65, 544), (64, 64, 512)])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 32), (1, 16, 128), (1, 33, 96), (2, 17, 160), (3, 100, 1024), (16, 64, 256), (17, 48, 2080), (5, 130, 4128), (40, 65, 544), (64, 64, 512),
+                                   (65, 33, 32), (96, 80, 160), (130, 257, 96), (200, 129, 480), (257, 300, 352), (520, 260, 128), (300, 270, 32), (256, 256, 608)])
 def test_product_shapes(m, n, k, at, fmt):
     rng = np.random.default_rng(m * n + k)
     ops = make_operands(rng, m, n, k, at, fmt)

@@ -592,6 +592,9 @@ mmaemu_status mmaemu_quantize_fp4(const void *x, void *codes, void *scales, void
 mmaemu_status mmaemu_matmul_fp4(const void *A, const void *SA, const void *W, const void *SW, void *D, uint32_t m, uint32_t n,
                                 uint32_t k, uint64_t a_stride, uint64_t d_stride, mmaemu_dtype a_type, mmaemu_dtype d_type,
                                 uint32_t scale_format, float alpha, void *hip_stream);
+/* Name of the kernel that mmaemu_matmul_fp4 takes for these sizes and types ("stream", or "blocks of 256 x 256" and smaller): decided on
+ * the host, no GPU needed; for tests and reports. */
+mmaemu_status mmaemu_matmul_fp4_kernel(uint32_t m, uint32_t n, uint32_t k, mmaemu_dtype a_type, uint32_t scale_format, const char **name);
 
 /*
  * Issue-rate probes: the measured counterpart of the vector-ALU peak that the emulation kernels' roofline is quoted

@@ -145,6 +145,7 @@ _lib.mmaemu_deviation_sample_kernel.argtypes = [_vp, _vp, _vp, _vp, _u32, _u32, 
 _lib.mmaemu_rmsnorm_quantize.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _u64, _u32, _u64, _u64, ctypes.c_int, ctypes.c_int, ctypes.c_int, _u32, ctypes.c_double, _vp]
 _lib.mmaemu_quantize_fp4.argtypes = [_vp, _vp, _vp, _vp, _u64, _u32, _u64, ctypes.c_int, _u32, _u32, ctypes.c_float, _vp]
 _lib.mmaemu_matmul_fp4.argtypes = [_vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u64, _u64, ctypes.c_int, ctypes.c_int, _u32, ctypes.c_float, _vp]
+_lib.mmaemu_matmul_fp4_kernel.argtypes = [_u32, _u32, _u32, ctypes.c_int, _u32, ctypes.POINTER(ctypes.c_char_p)]
 
 
 def _status_string(s):
@@ -340,6 +341,13 @@ def matmul_fp4(A, SA, W, SW, D, m, n, k, a_type, d_type, scale_format=SCALE_FORM
     """D = alpha A W^T with packed FP4 weights; SA: the activations' scales (8-bit types) or None."""
     _check(_lib.mmaemu_matmul_fp4(_ptr(A), _ptr(SA), _ptr(W), _ptr(SW), _ptr(D), m, n, k, a_stride, d_stride, a_type, d_type, scale_format, alpha,
                                   _stream(stream)))
+
+
+def matmul_fp4_kernel(m, n, k, a_type, scale_format=SCALE_FORMAT_E8M0):
+    """Name of the kernel that matmul_fp4 takes for these sizes and types; nothing is launched."""
+    name = ctypes.c_char_p()
+    _check(_lib.mmaemu_matmul_fp4_kernel(m, n, k, a_type, scale_format, ctypes.byref(name)))
+    return name.value.decode()
 
 
 # ---- unpacking of the device-side result structs (host copies; no arithmetic) -----------

@@ -917,9 +917,9 @@ mmaemu_status mmaemu_quantize_fp4(const void *x, void *codes, void *scales, void
     return launch_quantize_fp4(x, codes, scales, values, rows, cols, x_stride, type, scale_format, scale_rule, tensor_scale, (hipStream_t)hip_stream);
 }
 
-mmaemu_status mmaemu_matmul_fp4(const void *A, const void *SA, const void *W, const void *SW, void *D, uint32_t m, uint32_t n, uint32_t k,
-                                uint64_t a_stride, uint64_t d_stride, mmaemu_dtype a_type, mmaemu_dtype d_type, uint32_t scale_format, float alpha,
-                                void *hip_stream)
+// the checks that need no pointer; strides of 0 become the rows' lengths
+static mmaemu_status check_matmul_fp4(uint32_t m, uint32_t n, uint32_t k, uint64_t &a_stride, uint64_t &d_stride, uint32_t a_type, uint32_t d_type,
+                                      uint32_t scale_format, float alpha)
 {
     const bool bytes = a_type == MMAEMU_FP8_E4M3 || a_type == MMAEMU_FP8_E5M2;
     if (!bytes && a_type != MMAEMU_BF16 && a_type != MMAEMU_FP16) { set_error("matmul_fp4: activations are BF16, FP16, E4M3 or E5M2"); return MMAEMU_ERR_UNSUPPORTED; }
@@ -932,6 +932,16 @@ mmaemu_status mmaemu_matmul_fp4(const void *A, const void *SA, const void *W, co
     if (a_stride == 0) a_stride = k;
     if (d_stride == 0) d_stride = n;
     if (a_stride < k || d_stride < n || a_stride > (1ull << 38) || d_stride > (1ull << 38)) { set_error("matmul_fp4: a stride below its row's length or above 2^38"); return MMAEMU_ERR_SHAPE; }
+    return MMAEMU_OK;
+}
+
+mmaemu_status mmaemu_matmul_fp4(const void *A, const void *SA, const void *W, const void *SW, void *D, uint32_t m, uint32_t n, uint32_t k,
+                                uint64_t a_stride, uint64_t d_stride, mmaemu_dtype a_type, mmaemu_dtype d_type, uint32_t scale_format, float alpha,
+                                void *hip_stream)
+{
+    const mmaemu_status st = check_matmul_fp4(m, n, k, a_stride, d_stride, a_type, d_type, scale_format, alpha);
+    if (st != MMAEMU_OK) return st;
+    const bool bytes = is_byte_type(a_type);
     if (m == 0) return MMAEMU_OK;
     if (!A || !W || !SW || !D || (bytes && !SA)) { set_error("matmul_fp4: NULL device pointer"); return MMAEMU_ERR_INVALID_ARG; }
     if (!bytes && SA) { set_error("matmul_fp4: 16-bit activations take no scales"); return MMAEMU_ERR_INVALID_ARG; }
@@ -940,6 +950,16 @@ mmaemu_status mmaemu_matmul_fp4(const void *A, const void *SA, const void *W, co
         return MMAEMU_ERR_INVALID_ARG;
     }
     return launch_matmul_fp4(A, SA, W, SW, D, m, n, k, a_stride, d_stride, a_type, d_type, scale_format, alpha, (hipStream_t)hip_stream);
+}
+
+mmaemu_status mmaemu_matmul_fp4_kernel(uint32_t m, uint32_t n, uint32_t k, mmaemu_dtype a_type, uint32_t scale_format, const char **name)
+{
+    if (!name) { set_error("matmul_fp4_kernel: NULL pointer"); return MMAEMU_ERR_INVALID_ARG; }
+    uint64_t a_stride = 0, d_stride = 0;
+    const mmaemu_status st = check_matmul_fp4(m, n, k, a_stride, d_stride, a_type, MMAEMU_FP32, scale_format, 1.0f);
+    if (st != MMAEMU_OK) return st;
+    *name = matmul_fp4_kernel_name(m, n, a_type, scale_format);
+    return MMAEMU_OK;
 }
 
 } // extern "C"

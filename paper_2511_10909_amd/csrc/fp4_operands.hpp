@@ -94,6 +94,21 @@ template <int AT> __device__ __forceinline__ f32x4 mfma_scaled(u32x4 w, uint32_t
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, x, c, 4, AT == MMAEMU_FP8_E5M2 ? 1 : 0, 0, (int)sw, 0, (int)sx);
 }
 
+__device__ __forceinline__ uint32_t lds_address(const uint8_t *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p; }
+
+// Sixteen bytes per lane from memory to LDS, to + 16 lane.  By hand: before a read the compiler waits for every copy that it
+// knows of, as it cannot tell the buffers apart.  No register is written, and the address is read as the copy is issued.
+__device__ __forceinline__ void copy_to_lds(const uint8_t *from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+
+// the same for one aligned word per lane, to + 4 lane
+__device__ __forceinline__ void copy_word_to_lds(const uint8_t *from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
+}
+
 struct ProductArgs {
     const uint8_t *A, *SA, *W, *SW;
     void *D;
@@ -105,6 +120,7 @@ struct ProductArgs {
 
 // the kernel for many rows of A (matmul_fp4_tiled.hip)
 mmaemu_status launch_tiled(const ProductArgs &p, uint32_t a_type, uint32_t scale_format, hipStream_t s);
+const char *tiled_name(uint32_t m, uint32_t n, uint32_t a_type, uint32_t scale_format);
 
 // four consecutive outputs of one token, columns j .. j + 3, in type DT
 template <int DT> __device__ __forceinline__ void store_outputs(const ProductArgs &p, uint32_t i, uint32_t j, f32x4 v)

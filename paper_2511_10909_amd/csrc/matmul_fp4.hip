@@ -4,110 +4,244 @@
 
 namespace mmaemu {
 
-constexpr int STREAM_WAVES = 8;
+// Few tokens: the weights are read once, by the wavefront that multiplies them; nothing is shared but the sum.  A workgroup's
+// wavefronts take the same 16 tokens x 16 NT weight rows and each a contiguous part of the products; their sums meet in LDS.
+//
+// Each wavefront keeps a ring of R slots of DW windows in LDS that only it uses: copies by the memory system fill the slots
+// ahead, and no barrier is needed.  Loads straight into registers are slower: the instructions want sixteen rows in
+// consecutive lanes, and the first-level cache looks up a line for each lane then, 64 for a load; the copies run along the rows.
+template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> struct Stream {
+    static constexpr bool BYTES = AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2;
+    static constexpr int XB = BYTES ? 128 : 256;                       // bytes of a token per window
+    static constexpr int WROW = 64 * DW;                               // bytes of a weight row per slot
+    static constexpr int SB = SF == MMAEMU_SCALE_FORMAT_E8M0 ? 4 : 8;  // scale bytes of a weight row per window
+    static constexpr int W_BYTES = 16 * NT * WROW, X_BYTES = DW * MR * XB, SLOT = W_BYTES + X_BYTES;
+    static constexpr int WC = W_BYTES / 1024, XC = (X_BYTES + 1023) / 1024, COPIES = WC + XC;
+    static constexpr int RUN = 16;                                     // windows whose scales are staged together
+    static constexpr int SW_ROW = RUN * SB, SX_ROW = RUN * 4;          // bytes of a row's scales in a run
+    static constexpr int SW_BYTES = 16 * NT * SW_ROW, SX_BYTES = BYTES ? MR * SX_ROW : 0;
+    static constexpr int WAVE_LDS = R * SLOT + SW_BYTES + SX_BYTES;
+    static constexpr int SUM_LDS = NT * WAVES * 1024;
+    static constexpr int LDS = WAVES * WAVE_LDS > SUM_LDS ? WAVES * WAVE_LDS : SUM_LDS;
+};
 
-// the activations of one window, and its products
-template <int AT, int SF>
-__device__ __forceinline__ f32x4 window(const ProductArgs &p, const uint8_t *arow, const uint8_t *sarow, const uint8_t *wrow, const uint8_t *swrow,
-                                        uint32_t k0, uint32_t g, f32x4 acc)
+// one window: weights w with scales s, MT x XW pieces of activations
+template <int AT, int SF> __device__ __forceinline__ f32x4 window_products(u32x4 w, uint32_t s, const u32x4 (&x)[AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2 ? 2 : 4], uint32_t sx, f32x4 acc)
 {
-    const bool in = k0 + 32 * g < p.k;             // k is a multiple of 32: a block is inside as a whole
-    u32x4 w = {0, 0, 0, 0};
-    if (in) w = *reinterpret_cast<const u32x4 *>(wrow + (k0 + 32 * g) / 2);
     if constexpr (AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2) {
-        uint32_t sw = 127, sx = 127;
-        if (in) {
-            sw = swrow[k0 / 32 + g];
-            sx = sarow[k0 / 32 + g];
-        }
-        i32x8 x = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t kx = k0 + 64 * h + 16 * g;
-            if (kx < p.k) {
-                const u32x4 v = *reinterpret_cast<const u32x4 *>(arow + kx);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) x[4 * h + q] = (int)v[q];
-            }
-        }
-        return mfma_scaled<AT>(w, sw, x, sx, acc);
-    } else {
-        Frag16 x[4];
+        const i32x8 v = {(int)x[0][0], (int)x[0][1], (int)x[0][2], (int)x[0][3], (int)x[1][0], (int)x[1][1], (int)x[1][2], (int)x[1][3]};
+        return mfma_scaled<AT>(w, s, v, sx, acc);
+    } else if constexpr (SF == MMAEMU_SCALE_FORMAT_UE4M3) {
+        const f16x2 sh = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(s & 0x7F7Fu, 1.0f, 0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            x[j].w = u32x4{0, 0, 0, 0};
-            if (in) x[j].w = *reinterpret_cast<const u32x4 *>(arow + 2 * (k0 + 32 * g) + 16 * j);
+            const _Float16 sj = sh[j / 2];
+            if constexpr (AT == MMAEMU_FP16) acc = mfma_fp16(weights_fp16_by(w[j], f16x2{sj, sj}), Frag16{x[j]}, acc);
+            else acc = mfma_bf16(weights_bf16_by(w[j], (float)sj), Frag16{x[j]}, acc);
         }
-        if constexpr (SF == MMAEMU_SCALE_FORMAT_E8M0) {
-            const uint32_t sw = in ? swrow[k0 / 32 + g] : 127u;
-            if (AT == MMAEMU_FP16 && __all(fp16_holds(sw))) {
+    } else if (AT == MMAEMU_BF16 || !__all(fp16_holds(s))) {
+        const bool far = AT == MMAEMU_FP16 && s - 253u < 2u;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc = mfma_fp16(weights_fp16(w[j], sw), x[j], acc);
+        for (int j = 0; j < 4; ++j) {
+            const Frag16 f = weights_bf16(w[j], far ? s - 2 : s);
+            if (AT == MMAEMU_FP16) {
+                Frag16 hi, lo;
+                split_fp16(Frag16{x[j]}, far ? 4.0f : 1.0f, hi, lo);
+                acc = mfma_bf16(f, lo, acc);
+                acc = mfma_bf16(f, hi, acc);
+                __builtin_amdgcn_sched_barrier(0);                     // (rare: the parts of one piece at a time in registers)
+            } else acc = mfma_bf16(f, Frag16{x[j]}, acc);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc = mfma_fp16(weights_fp16(w[j], s), Frag16{x[j]}, acc);
+    }
+    return acc;
+}
+
+template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ void __launch_bounds__(64 * WAVES) stream_kernel(const ProductArgs p)
+{
+    typedef Stream<AT, SF, MR, NT, DW, R, WAVES> T;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15u;
+    const uint32_t n0 = blockIdx.x * (16 * NT);
+    uint8_t *const ring = lds + wave * T::WAVE_LDS, *const sw_lds = ring + R * T::SLOT, *const sx_lds = sw_lds + T::SW_BYTES;
+    // this wavefront's slots of the row
+    const uint32_t slots = (p.k + 128 * DW - 1) / (128 * DW), per = slots / WAVES, more = slots % WAVES;
+    const uint32_t first = wave * per + (wave < more ? wave : more), count = per + (wave < more ? 1 : 0);
+
+    // Sources of this lane's copies.  Rows of 128 bytes and more are stored with their 16-byte chunks rotated, so that the lanes
+    // that read together find them in different banks.
+    const uint8_t *src[T::COPIES];
+    uint32_t src_k[T::COPIES];                     // products before the chunk, within the slot
+    bool src_in[T::COPIES];
+#pragma unroll
+    for (int i = 0; i < T::WC; ++i) {
+        const uint32_t chunk = 64 * i + lane, row = chunk / (4 * DW), pos = chunk % (4 * DW);
+        const uint32_t c = DW == 2 ? pos ^ ((row >> 1) & 7) : pos ^ ((row >> 2) & 3);
+        const uint32_t n = n0 + row < p.n ? n0 + row : p.n - 1;
+        src[i] = p.W + (uint64_t)n * (p.k / 2) + (uint64_t)first * T::WROW + 16 * c;
+        src_k[i] = 32 * c;
+        src_in[i] = true;
+    }
+#pragma unroll
+    for (int i = 0; i < T::XC; ++i) {
+        constexpr uint32_t PER_ROW = T::XB / 16;
+        const uint32_t chunk = 64 * i + lane, win = chunk / (MR * PER_ROW), row = chunk / PER_ROW % MR, pos = chunk % PER_ROW;
+        const uint32_t c = pos ^ (T::BYTES ? (row >> 1) & 7 : row & 15);
+        const uint32_t m = row;
+        src_in[T::WC + i] = chunk < (uint32_t)T::X_BYTES / 16;          // (tokens that are not there: the last one again)
+        src[T::WC + i] = p.A + (uint64_t)(m < p.m ? m : p.m - 1) * p.a_stride + (uint64_t)first * (DW * T::XB) + win * T::XB + 16 * c;
+        src_k[T::WC + i] = 128 * win + (T::BYTES ? 16 : 8) * c;
+    }
+    auto issue = [&](uint32_t d) {                 // the copies of this wavefront's slot d
+        const uint32_t slot = lds_address(ring) + (d % R) * T::SLOT;
+        if ((first + d + 1) * (128 * DW) > p.k) {
+            // the slot that ends inside: zeros first, then what is there
+            for (uint32_t c = lane; c < (uint32_t)T::SLOT / 16; c += 64) *reinterpret_cast<u32x4 *>(ring + (d % R) * T::SLOT + 16 * c) = u32x4{0, 0, 0, 0};
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < T::COPIES; ++i)
+                if (src_in[i] && (first + d) * (128 * DW) + src_k[i] < p.k) copy_to_lds(src[i] + (uint64_t)d * (i < T::WC ? T::WROW : DW * T::XB), slot + (i < T::WC ? 1024 * i : T::W_BYTES + 1024 * (i - T::WC)));
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < T::WC; ++i) copy_to_lds(src[i] + (uint64_t)d * T::WROW, slot + 1024 * i);
+#pragma unroll
+        for (int i = 0; i < T::XC; ++i)
+            if (src_in[T::WC + i]) copy_to_lds(src[T::WC + i] + (uint64_t)d * (DW * T::XB), slot + T::W_BYTES + 1024 * i);
+    };
+    // scales of sixteen windows from this wavefront's slot d on: sixteen bytes per lane, byte by byte at a row's end
+    auto stage_scales = [&](uint32_t d) {
+        constexpr uint32_t PIECES = (16 * NT * T::SW_ROW + T::SX_BYTES) / 16;
+        const uint32_t w0 = (first + d) * DW;      // first window
+#pragma unroll
+        for (uint32_t q0 = 0; q0 < PIECES; q0 += 64) {
+            const uint32_t q = q0 + lane;
+            if (PIECES % 64 && q >= PIECES) break;
+            const bool of_w = q < (uint32_t)T::SW_BYTES / 16;
+            const uint32_t x = q - T::SW_BYTES / 16, row = of_w ? q / (T::SW_ROW / 16) : x / (T::SX_ROW / 16), at = 16 * (of_w ? q % (T::SW_ROW / 16) : x % (T::SX_ROW / 16));
+            const uint32_t n = n0 + row < p.n ? n0 + row : p.n - 1, m = row < p.m ? row : p.m - 1;
+            const uint32_t all = of_w ? p.k / (128 / T::SB) : p.k / 32, begin = w0 * (of_w ? T::SB : 4) + at;
+            const uint8_t *from = (of_w ? p.SW + (uint64_t)n * all : p.SA + (uint64_t)m * all) + begin;
+            Words4<1> v;
+            if (begin + 16 <= all) v = *reinterpret_cast<const Words4<1> *>(from);
+            else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v.w[e] = SF == MMAEMU_SCALE_FORMAT_UE4M3 ? 0x38383838u : 0x7F7F7F7Fu;
+#pragma unroll
+                for (uint32_t e = 0; e < 15; ++e)
+                    if (begin + e < all) v.w[e / 4] = (v.w[e / 4] & ~(0xFFu << (8 * (e % 4)))) | (uint32_t)from[e] << (8 * (e % 4));
+            }
+            *reinterpret_cast<u32x4 *>((of_w ? sw_lds : sx_lds - T::SW_BYTES) + 16 * q) = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+        }
+    };
+
+    const bool ends_inside = (first + count) * (128 * DW) > p.k;
+    f32x4 acc[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j] = f32x4{0, 0, 0, 0};
+    for (uint32_t d = 0; d < R && d < count; ++d) issue(d);
+    for (uint32_t d = 0; d < count; ++d) {
+        if (d % (T::RUN / DW) == 0) stage_scales(d);
+        // slots that may still be under way (one that ends inside counts as none: it may have fewer copies)
+        const uint32_t left = count - d - 1, later = left < R - 1 ? left : R - 1, away = later && later == left && ends_inside ? later - 1 : later;
+        if (away >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * T::COPIES) : "memory");
+        else if (away == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * T::COPIES) : "memory");
+        else if (away == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::COPIES) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const uint8_t *slot = ring + (d % R) * T::SLOT, *xs = slot + T::W_BYTES;
+        const uint32_t rx = r % MR;
+#pragma unroll
+        for (int h = 0; h < DW; ++h) {
+            const uint32_t win = d % (T::RUN / DW) * DW + h;
+            u32x4 x[T::BYTES ? 2 : 4];
+            uint32_t sx = 0;
+            if constexpr (T::BYTES) {
+                const uint8_t *row = xs + (h * MR + rx) * 128;
+                const uint32_t rot = (rx >> 1) & 7;
+                x[0] = *reinterpret_cast<const u32x4 *>(row + 16 * (g ^ rot));
+                x[1] = *reinterpret_cast<const u32x4 *>(row + 16 * ((4 + g) ^ rot));
+                sx = sx_lds[rx * T::SX_ROW + 4 * win + g];
             } else {
+                const uint8_t *row = xs + (h * MR + rx) * 256;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (AT == MMAEMU_FP16) {
-                        const bool far = sw - 253u < 2u;
-                        const Frag16 f = weights_bf16(w[j], far ? sw - 2 : sw);
-                        Frag16 hi, lo;
-                        split_fp16(x[j], far ? 4.0f : 1.0f, hi, lo);
-                        acc = mfma_bf16(f, lo, acc);
-                        acc = mfma_bf16(f, hi, acc);
-                    } else acc = mfma_bf16(weights_bf16(w[j], sw), x[j], acc);
-                }
+                for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const u32x4 *>(row + 16 * ((4 * g + j) ^ rx));
             }
-        } else {
-            uint32_t s = 0;
-            if (in) s = (swrow[k0 / 16 + 2 * g] & 0x7Fu) | (swrow[k0 / 16 + 2 * g + 1] & 0x7Fu) << 8;
-            const f16x2 sh = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(s, 1.0f, 0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const _Float16 sj = sh[j / 2];
-                if (AT == MMAEMU_FP16) acc = mfma_fp16(weights_fp16_by(w[j], f16x2{sj, sj}), x[j], acc);
-                else acc = mfma_bf16(weights_bf16_by(w[j], (float)sj), x[j], acc);
+            for (int j = 0; j < NT; ++j) {
+                const uint32_t c = DW == 2 ? (4 * h + g) ^ ((r >> 1) & 7) : g ^ (r >> 2);
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(slot + (16 * j + r) * T::WROW + 16 * c);
+                const uint8_t *sr = sw_lds + (16 * j + r) * T::SW_ROW + T::SB * win;
+                const uint32_t sc = SF == MMAEMU_SCALE_FORMAT_E8M0 ? sr[g] : *reinterpret_cast<const uint16_t *>(sr + 2 * g);
+                acc[j] = window_products<AT, SF>(w, sc, x, sx, acc[j]);
             }
         }
-        return acc;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // everything of the slot has been read
+        if (d + R < count) issue(d + R);
+    }
+    __syncthreads();
+    f32x4 *part = reinterpret_cast<f32x4 *>(lds);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) part[(j * WAVES + wave) * 64 + lane] = acc[j];
+    __syncthreads();
+    for (uint32_t t = wave; t < NT; t += WAVES) {
+        f32x4 sum = part[t * WAVES * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) sum += part[(t * WAVES + w) * 64 + lane];
+        with_output_type(p.d_type, [&](auto dt) { store_outputs<dt.value>(p, r, n0 + 16 * t + 4 * g, sum); });
     }
 }
 
-template <int AT, int SF> __global__ void __launch_bounds__(64 * STREAM_WAVES) stream_kernel(const ProductArgs p)
+template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> static mmaemu_status launch_stream(const ProductArgs &p, hipStream_t s)
 {
-    __shared__ f32x4 part[STREAM_WAVES][64];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, g = lane >> 4;
-    const uint32_t n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
-    const uint32_t j = n0 + (lane & 15u) < p.n ? n0 + (lane & 15u) : p.n - 1, i = m0 + (lane & 15u) < p.m ? m0 + (lane & 15u) : p.m - 1;
-    const uint8_t *wrow = p.W + (uint64_t)j * (p.k / 2), *swrow = p.SW + (uint64_t)j * (p.k / (SF == MMAEMU_SCALE_FORMAT_E8M0 ? 32 : 16));
-    const uint8_t *arow = p.A + (uint64_t)i * p.a_stride, *sarow = p.SA + (uint64_t)i * (p.k / 32);
-    f32x4 acc = {0, 0, 0, 0};
-    for (uint32_t k0 = 128 * wave; k0 < p.k; k0 += 128 * STREAM_WAVES) acc = window<AT, SF>(p, arow, sarow, wrow, swrow, k0, g, acc);
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (wave) return;
-#pragma unroll
-    for (int w = 1; w < STREAM_WAVES; ++w) acc += part[w][lane];
-    with_output_type(p.d_type, [&](auto dt) { store_outputs<dt.value>(p, m0 + (lane & 15u), n0 + 4 * g, acc); });
-}
-
-template <int AT, int SF> static mmaemu_status launch_product(const ProductArgs &p, hipStream_t s)
-{
-    hipLaunchKernelGGL((stream_kernel<AT, SF>), dim3((p.n + 15) / 16, (p.m + 15) / 16), dim3(64 * STREAM_WAVES), 0, s, p);
+    typedef Stream<AT, SF, MR, NT, DW, R, WAVES> T;
+    static_assert(T::LDS <= 160 * 1024 && R <= 4, "ring");
+    hipLaunchKernelGGL((stream_kernel<AT, SF, MR, NT, DW, R, WAVES>), dim3((p.n + 16 * NT - 1) / (16 * NT)), dim3(64 * WAVES), T::LDS, s, p);
     MMAEMU_HIP(hipGetLastError());
     return MMAEMU_OK;
+}
+
+// Up to sixteen tokens go through the stream (32 x 32 blocks take 14 us against 10.4 for 16 BF16 tokens on 8192 x 8192 MXFP4 weights, 10.9
+// against 8.9 for E4M3 ones; at 32 tokens the stream reads the weights twice).
+constexpr uint32_t STREAM_TOKENS = 16;
+
+// Rows of a slot's activations: those that the tokens fill, 4, 8 (16-bit ones) or 16; fewer cost less of the copies' rate (one BF16 token on
+// 28672 x 8192: 24 us with 2 rows, 37 with 16).  Weight rows: 16 a workgroup until they fill the chip, then more, which share the activations (16 BF16 tokens,
+// n = 4096 / 8192 / 28672, k = 4096 / 8192 / 8192: 5.5, 12.4 and 45 us with 16; 7.3, 10.5 and 39 with 32; 9.9, 13.7 and 33 with 64).  Eight
+// wavefronts instead of four where few workgroups share long rows (one BF16 token, 1024 x 16384: 8.4 -> 6.4 us; 28672 x 8192: 23.8 -> 26.3).
+template <int AT, int SF> static mmaemu_status launch_stream_typed(const ProductArgs &p, hipStream_t s)
+{
+    const bool few = p.n < 4096 && p.k >= 4096;
+    if (p.m <= 4) return few ? launch_stream<AT, SF, 4, 1, 2, 2, 8>(p, s) : launch_stream<AT, SF, 4, 1, 2, 2, 4>(p, s);
+    if constexpr (AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2) {
+        if (p.n > 4096) return launch_stream<AT, SF, 16, 2, 2, 2, 4>(p, s);
+        return few ? launch_stream<AT, SF, 16, 1, 2, 2, 8>(p, s) : launch_stream<AT, SF, 16, 1, 2, 2, 4>(p, s);
+    } else {
+        if (p.m <= 8) return p.n < 16384 ? launch_stream<AT, SF, 8, 1, 2, 2, 4>(p, s) : launch_stream<AT, SF, 8, 2, 2, 2, 4>(p, s);
+        if (p.n <= 4096) return launch_stream<AT, SF, 16, 1, 1, 2, 8>(p, s);
+        return p.n < 16384 || p.k < 2048 ? launch_stream<AT, SF, 16, 2, 1, 2, 4>(p, s) : launch_stream<AT, SF, 16, 4, 1, 2, 4>(p, s);
+    }
 }
 
 mmaemu_status launch_matmul_fp4(const void *A, const void *SA, const void *W, const void *SW, void *D, uint32_t m, uint32_t n, uint32_t k,
                                 uint64_t a_stride, uint64_t d_stride, uint32_t a_type, uint32_t d_type, uint32_t scale_format, float alpha, hipStream_t s)
 {
-    const bool bytes = a_type == MMAEMU_FP8_E4M3 || a_type == MMAEMU_FP8_E5M2;
+    const bool bytes = is_byte_type(a_type), e8m0 = scale_format == MMAEMU_SCALE_FORMAT_E8M0;
     const ProductArgs p = {(const uint8_t *)A, (const uint8_t *)SA, (const uint8_t *)W, (const uint8_t *)SW, D, a_stride * (bytes ? 1 : 2), d_stride, m, n, k,
                            d_type, alpha};
-    if (m >= 256) return launch_tiled(p, a_type, scale_format, s);
-    if (a_type == MMAEMU_FP8_E4M3) return launch_product<MMAEMU_FP8_E4M3, MMAEMU_SCALE_FORMAT_E8M0>(p, s);
-    if (a_type == MMAEMU_FP8_E5M2) return launch_product<MMAEMU_FP8_E5M2, MMAEMU_SCALE_FORMAT_E8M0>(p, s);
-    if (scale_format == MMAEMU_SCALE_FORMAT_E8M0)
-        return a_type == MMAEMU_BF16 ? launch_product<MMAEMU_BF16, MMAEMU_SCALE_FORMAT_E8M0>(p, s) : launch_product<MMAEMU_FP16, MMAEMU_SCALE_FORMAT_E8M0>(p, s);
-    return a_type == MMAEMU_BF16 ? launch_product<MMAEMU_BF16, MMAEMU_SCALE_FORMAT_UE4M3>(p, s) : launch_product<MMAEMU_FP16, MMAEMU_SCALE_FORMAT_UE4M3>(p, s);
+    if (m > STREAM_TOKENS) return launch_tiled(p, a_type, scale_format, s);
+    switch (a_type) {
+    case MMAEMU_FP8_E4M3: return launch_stream_typed<MMAEMU_FP8_E4M3, MMAEMU_SCALE_FORMAT_E8M0>(p, s);
+    case MMAEMU_FP8_E5M2: return launch_stream_typed<MMAEMU_FP8_E5M2, MMAEMU_SCALE_FORMAT_E8M0>(p, s);
+    case MMAEMU_BF16: return e8m0 ? launch_stream_typed<MMAEMU_BF16, MMAEMU_SCALE_FORMAT_E8M0>(p, s) : launch_stream_typed<MMAEMU_BF16, MMAEMU_SCALE_FORMAT_UE4M3>(p, s);
+    default: return e8m0 ? launch_stream_typed<MMAEMU_FP16, MMAEMU_SCALE_FORMAT_E8M0>(p, s) : launch_stream_typed<MMAEMU_FP16, MMAEMU_SCALE_FORMAT_UE4M3>(p, s);
+    }
+}
+
+const char *matmul_fp4_kernel_name(uint32_t m, uint32_t n, uint32_t a_type, uint32_t scale_format)
+{
+    return m > STREAM_TOKENS ? tiled_name(m, n, a_type, scale_format) : "stream";
 }
 
 } // namespace mmaemu

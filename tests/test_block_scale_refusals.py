@@ -61,3 +61,11 @@ def test_no_rows_is_no_work():
     mm.rmsnorm_quantize(None, None, None, None, None, None, 0, 64, mm.BF16, mm.BF16, mm.E4M3, stream=0)
     mm.quantize_fp4(None, None, None, None, 0, 64, mm.BF16, stream=0)
     mm.matmul_fp4(None, None, None, None, None, 0, 8, 64, mm.BF16, mm.BF16, stream=0)
+
+
+def test_kernel_names_of_products():
+    assert mm.matmul_fp4_kernel(1, 4096, 4096, mm.BF16) == "stream" and mm.matmul_fp4_kernel(8192, 8192, 8192, mm.E4M3) == "blocks of 256 x 256"
+    for status, args in ((SHAPE, (1, 0, 32, mm.BF16)), (SHAPE, (1, 8, 33, mm.BF16)), (UNSUPPORTED, (1, 8, 32, mm.FP32)), (UNSUPPORTED, (1, 8, 32, mm.E4M3, 1))):
+        with pytest.raises(mm.MmaemuError) as e:
+            mm.matmul_fp4_kernel(*args)
+        assert e.value.status == status

@@ -413,3 +413,68 @@ def test_chain_on_a_stream_and_in_a_graph():
         av = bs.values_of(qc, mm.E4M3) * np.repeat(np.exp2(qs.astype(np.float64) - 127), 32, axis=1)
         got = bs.values_of(host(D, np.uint32, (m, n)), mm.FP32)
         assert (np.abs(got - av @ wv.T) <= product_bound(av, wv, mm.E4M3) + np.abs(av @ wv.T) * 2.0 ** -23).all()
+
+
+KERNELS = [("stream", 1, 30), ("stream", 4, 4097), ("stream", 5, 100), ("stream", 8, 16401), ("stream", 9, 70), ("stream", 16, 4110), ("stream", 13, 16390),
+           ("blocks of 32 x 32", 17, 40), ("blocks of 32 x 64", 77, 5003), ("blocks of 64 x 64", 250, 4093), ("blocks of 128 x 128", 500, 8190),
+           ("blocks of 128 x 256", 250, 28000), ("blocks of 256 x 256", 4090, 4085)]
+
+
+@pytest.mark.parametrize("at,fmt", AT_FMT)
+@pytest.mark.parametrize("name,m,n", KERNELS)
+def test_product_every_kernel(name, m, n, at, fmt):
+    """Every kernel, at sizes that its blocks do not divide and products that end inside a step, or do not fill one: every output against the
+    sum of the magnitudes, and some against the bound of their own products."""
+    if not (name == "blocks of 256 x 256" and at == mm.FP16 and fmt == bs.SCALE_E8M0):
+        assert mm.matmul_fp4_kernel(m, n, 32, at, fmt) == name
+    rng = np.random.default_rng(m + n)
+    for k in (32, 416, 1024, 2144):
+        if m * n * k > 1 << 33:
+            continue
+        A, SA, W, SW, av, wv = make_operands(rng, m, n, k, at, fmt)
+        got = bs.values_of(run_product(A, SA, W, SW, n, at, mm.FP32, fmt, 0.5), mm.FP32)
+        want, total = 0.5 * (av @ wv.T), 0.5 * (np.abs(av) @ np.abs(wv).T)
+        loose = ((k / 8 + 40) * 2.0 ** -23 + 8 * (2.0 ** -23 if SA is None else 2.0 ** -13)) * total
+        assert (np.abs(got - want) <= loose + np.abs(want) * 2.0 ** -23).all()
+        i, j = rng.integers(0, m, 24), rng.integers(0, n, 24)
+        i[0], j[0], i[1], j[1] = m - 1, n - 1, 0, n - 1
+        tight = 0.5 * product_bound(av[i], wv[j], at)
+        d = np.abs(got[np.ix_(i, j)] - want[np.ix_(i, j)])
+        assert (d <= tight + np.abs(want[np.ix_(i, j)]) * 2.0 ** -23).all(), float((d / tight).max())
+
+
+@pytest.mark.parametrize("m,n", [(17, 40), (77, 5003), (250, 4093), (500, 8190), (250, 28000)])
+def test_product_fp16_weights_of_every_scale_in_blocks(m, n):
+    """FP16 activations where some E8M0 scales leave FP16's range: both ways in one product."""
+    rng = np.random.default_rng(3)
+    k = 544
+    A, SA, W, SW, av, wv = make_operands(rng, m, n, k, mm.FP16, bs.SCALE_E8M0, 100, 150)
+    SW[rng.random(SW.shape) < 0.9] = 120
+    wv = bs.weights(W, SW, bs.SCALE_E8M0)
+    got = bs.values_of(run_product(A, None, W, SW, n, mm.FP16, mm.FP32, bs.SCALE_E8M0), mm.FP32)
+    want, total = av @ wv.T, np.abs(av) @ np.abs(wv).T
+    # (the second way adds twice as many terms)
+    assert (np.abs(got - want) <= ((k / 4 + 40) * 2.0 ** -23 + 16 * 2.0 ** -23) * total + np.abs(want) * 2.0 ** -23).all()
+
+
+@pytest.mark.parametrize("at,fmt", AT_FMT)
+@pytest.mark.parametrize("m", [1, 16, 40, 300])
+def test_product_unaligned_scales(at, fmt, m):
+    """Scales at any byte, and rows of them of any length: the products' copies take aligned words."""
+    rng = np.random.default_rng(m)
+    n = 300
+    for k in (96, 1056, 4128):
+        A, SA, W, SW, av, wv = make_operands(rng, m, n, k, at, fmt)
+        D = torch.empty(m * n * 4, dtype=torch.uint8, device="cuda")
+        dA, dW = dev(A), dev(W)
+        want, total = av @ wv.T, np.abs(av) @ np.abs(wv).T
+        loose = ((k / 8 + 40) * 2.0 ** -23 + 8 * (2.0 ** -23 if SA is None else 2.0 ** -13)) * total + np.abs(want) * 2.0 ** -23
+        for off in (0, 1, 2, 3):
+            hold = [torch.full((s.size + 64,), 0xFF, dtype=torch.uint8, device="cuda") for s in ((SW,) if SA is None else (SW, SA))]      # NaN codes around the scales
+            for h, s in zip(hold, (SW, SA)):
+                h[off + 16:off + 16 + s.size] = dev(s)
+            sw, sa = hold[0][off + 16:], None if SA is None else hold[1][off + 16:]
+            mm.matmul_fp4(dA, sa, dW, sw, D, m, n, k, at, mm.FP32, fmt)
+            torch.cuda.synchronize()
+            got = bs.values_of(host(D, np.uint32, (m, n)), mm.FP32)
+            assert (np.abs(got - want) <= loose).all()

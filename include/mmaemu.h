@@ -585,7 +585,8 @@ mmaemu_status mmaemu_quantize_fp4(const void *x, void *codes, void *scales, void
  * d_type: FP32, BF16 or FP16 (nearest even, overflow gives infinities).  Rows of A are a_stride elements apart (0: k), those of
  * D d_stride (0: n).  A NaN scale makes the outputs of its row of A or W NaN.  D may not overlap the inputs.  m = 0 is a
  * no-op.  Forward only; one launch without workspace; the order of a sum depends on m, n, k and types only.
- * Errors: SHAPE (n or k zero, k not a multiple of 32, k > 2^20, a stride below its row, m or n > 2^24, a row stride over 2^40),
+ * Errors: SHAPE (n or k zero, k not a multiple of 32, k > 2^20, a stride below its row, over 2^22 for A or 2^38
+ *         for D, m or n > 2^24),
  *         INVALID_ARG (NULL pointers, scale format; A and W aligned to 16 bytes with rows of A a multiple of 16 bytes
  *         apart, D to its element size; alpha not finite; SA given for 16-bit activations), UNSUPPORTED (types; UE4M3 with 8-bit activations).
  */

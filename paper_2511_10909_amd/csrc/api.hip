@@ -931,7 +931,7 @@ static mmaemu_status check_matmul_fp4(uint32_t m, uint32_t n, uint32_t k, uint64
     if (m > (1u << 24) || n > (1u << 24)) { set_error("matmul_fp4: m or n above 2^24"); return MMAEMU_ERR_SHAPE; }
     if (a_stride == 0) a_stride = k;
     if (d_stride == 0) d_stride = n;
-    if (a_stride < k || d_stride < n || a_stride > (1ull << 38) || d_stride > (1ull << 38)) { set_error("matmul_fp4: a stride below its row's length or above 2^38"); return MMAEMU_ERR_SHAPE; }
+    if (a_stride < k || d_stride < n || a_stride > (1ull << 22) || d_stride > (1ull << 38)) { set_error("matmul_fp4: a stride below its row's length, or above 2^22 (A) or 2^38 (D)"); return MMAEMU_ERR_SHAPE; }
     return MMAEMU_OK;
 }
 

@@ -12,6 +12,9 @@
 #include "block_scale.hpp"
 #include <type_traits>
 
+// for lambdas of the kernels: one that is not inlined holds all that it names in scratch memory
+#define MMAEMU_INLINE __attribute__((always_inline))
+
 namespace mmaemu {
 
 // Weights of 16-bit activations are brought to the activations' type, scale included.  That is exact: E2M1 2^(code - 127) is
@@ -103,9 +106,20 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t *from, uint32_t to)
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
 }
 
-// the same for one aligned word per lane, to + 4 lane
+// the same from a uniform base
+__device__ __forceinline__ void copy_to_lds(const uint8_t *base, uint32_t from, uint32_t to)
+{
+    // (uniform in any case: the compiler may hold them in vector registers)
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32));
+    base = (const uint8_t *)((uintptr_t)hi << 32 | lo);
+    to = __builtin_amdgcn_readfirstlane(to);
+    // (five wait states between a vector instruction that may have written the base and its use)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(from), "s"(base), "s"(to) : "memory");
+}
+// one aligned word per lane, to + 4 lane
 __device__ __forceinline__ void copy_word_to_lds(const uint8_t *from, uint32_t to)
 {
+    to = __builtin_amdgcn_readfirstlane(to);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
 }
 

@@ -94,7 +94,7 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
         src[T::WC + i] = p.A + (uint64_t)(m < p.m ? m : p.m - 1) * p.a_stride + (uint64_t)first * (DW * T::XB) + win * T::XB + 16 * c;
         src_k[T::WC + i] = 128 * win + (T::BYTES ? 16 : 8) * c;
     }
-    auto issue = [&](uint32_t d) {                 // the copies of this wavefront's slot d
+    auto issue = [&](uint32_t d) MMAEMU_INLINE {                 // the copies of this wavefront's slot d
         const uint32_t slot = lds_address(ring) + (d % R) * T::SLOT;
         if ((first + d + 1) * (128 * DW) > p.k) {
             // the slot that ends inside: zeros first, then what is there
@@ -112,7 +112,7 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
             if (src_in[T::WC + i]) copy_to_lds(src[T::WC + i] + (uint64_t)d * (DW * T::XB), slot + T::W_BYTES + 1024 * i);
     };
     // scales of sixteen windows from this wavefront's slot d on: sixteen bytes per lane, byte by byte at a row's end
-    auto stage_scales = [&](uint32_t d) {
+    auto stage_scales = [&](uint32_t d) MMAEMU_INLINE {
         constexpr uint32_t PIECES = (16 * NT * T::SW_ROW + T::SX_BYTES) / 16;
         const uint32_t w0 = (first + d) * DW;      // first window
 #pragma unroll
@@ -202,7 +202,7 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> static mmaem
     return MMAEMU_OK;
 }
 
-// Up to sixteen tokens go through the stream (32 x 32 blocks take 14 us against 10.4 for 16 BF16 tokens on 8192 x 8192 MXFP4 weights, 10.9
+// Up to sixteen tokens go through the stream (32 x 32 blocks take 13 us against 10.5 for 16 BF16 tokens on 8192 x 8192 MXFP4 weights, 11
 // against 8.9 for E4M3 ones; at 32 tokens the stream reads the weights twice).
 constexpr uint32_t STREAM_TOKENS = 16;
 

@@ -41,100 +41,124 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
     const uint32_t t = die * per + (die < more ? die : more) + id / 8;
     const uint32_t band = 8 * tiles_n, b = t / band, inb = t - b * band, high = tiles_m - 8 * b < 8 ? tiles_m - 8 * b : 8;
     const uint32_t m0 = (8 * b + inb % high) * BM, n0 = (inb / high) * BN;
-    const uint32_t full = p.k / T::KS, steps = (p.k + T::KS - 1) / T::KS, row_scales = p.k / T::PER_SCALE;
+    const uint32_t steps = (p.k + T::KS - 1) / T::KS, row_scales = p.k / T::PER_SCALE;
+    const bool ends_inside = steps * T::KS > p.k;                      // the last step: products beyond the row are zero times zero
 
-    // Source of each of this thread's copies: part u, row, 16-byte chunk c of it.  Chunks are stored rotated by the row, so that
-    // the sixteen rows that lanes read together lie in different banks.
-    const uint8_t *src[T::COPIES];
-    auto chunk_of = [&](int i) -> uint32_t { return i < T::AC ? (i * T::THREADS + tid) % (T::A_BYTES / 16) : ((i - T::AC) * T::THREADS + tid) % (T::W_BYTES / 16); };
-    auto product_of = [&](int i) -> uint32_t {                         // the chunk's first product within the step
+    // Source of each of this thread's copies, from the block's first row: part, row, 16-byte chunk of it.  Chunks are stored rotated
+    // by the row, so that the sixteen rows that lanes read together lie in different banks.
+    uint32_t src[T::COPIES];
+    auto chunk_of = [&](int i) MMAEMU_INLINE -> uint32_t { return i < T::AC ? (i * T::THREADS + tid) % (T::A_BYTES / 16) : ((i - T::AC) * T::THREADS + tid) % (T::W_BYTES / 16); };
+    auto product_of = [&](int i) MMAEMU_INLINE -> uint32_t {                         // the chunk's first product within the step
         const uint32_t q = chunk_of(i);
         if (i < T::AC) return T::PART * (q / (T::A_PART / 16)) + (T::BYTES ? 16 : 8) * ((q % 8) ^ ((q / 16) & 7));
         return T::PART * (q / (T::W_PART / 16)) + 32 * (T::BYTES ? (q % 4) ^ ((q / 16) & 3) : q % 2);
     };
+    const uint32_t rows_m = p.m - m0 < BM ? p.m - m0 : BM, rows_n = p.n - n0 < BN ? p.n - n0 : BN;      // (rows beyond: the last one again)
 #pragma unroll
     for (int i = 0; i < T::COPIES; ++i) {
         if (i < T::AC) {
-            const uint32_t m = m0 + chunk_of(i) % (T::A_PART / 16) / 8;
-            src[i] = p.A + (uint64_t)(m < p.m ? m : p.m - 1) * p.a_stride + product_of(i) * (T::BYTES ? 1 : 2);
+            const uint32_t row = chunk_of(i) % (T::A_PART / 16) / 8;
+            src[i] = (row < rows_m ? row : rows_m - 1) * (uint32_t)p.a_stride + product_of(i) * (T::BYTES ? 1 : 2);
         } else {
-            const uint32_t n = n0 + chunk_of(i) % (T::W_PART / 16) / (T::WB / 16);
-            src[i] = p.W + (uint64_t)(n < p.n ? n : p.n - 1) * (p.k / 2) + product_of(i) / 2;
+            const uint32_t row = chunk_of(i) % (T::W_PART / 16) / (T::WB / 16);
+            src[i] = (row < rows_n ? row : rows_n - 1) * (p.k / 2) + product_of(i) / 2;
         }
     }
-    auto issue = [&](uint32_t s) {                                     // the copies of a whole step
-        const uint32_t to = lds_address(lds) + (s % S) * T::STAGE;
+    // The next step that copies are issued for: its place in both operands and in LDS.
+    const uint8_t *next_a = p.A + (uint64_t)m0 * p.a_stride, *next_w = p.W + (uint64_t)n0 * (p.k / 2);
+    uint32_t next_step = 0, next_at = 0;
+    auto issue = [&](bool whole) MMAEMU_INLINE {
+        auto place = [&](int i) MMAEMU_INLINE -> uint32_t {                          // of this wavefront's first chunk
+            return 16 * (i < T::AC ? (i * T::THREADS + 64 * wave) % (T::A_BYTES / 16) : T::A_BYTES / 16 + ((i - T::AC) * T::THREADS + 64 * wave) % (T::W_BYTES / 16));
+        };
+        if (whole) {
 #pragma unroll
-        for (int i = 0; i < T::COPIES; ++i) {
-            const uint32_t q = i < T::AC ? (i * T::THREADS + 64 * wave) % (T::A_BYTES / 16) : T::A_BYTES / 16 + ((i - T::AC) * T::THREADS + 64 * wave) % (T::W_BYTES / 16);
-            copy_to_lds(src[i] + (uint64_t)s * (i < T::AC ? 128 * WK : T::WB * WK), to + 16 * q);
+            for (int i = 0; i < T::COPIES; ++i) copy_to_lds(i < T::AC ? next_a : next_w, src[i], lds_address(lds) + next_at + place(i));
+        } else {
+#pragma unroll
+            for (int i = 0; i < T::COPIES; ++i) {
+                if (next_step * T::KS + product_of(i) < p.k) copy_to_lds(i < T::AC ? next_a : next_w, src[i], lds_address(lds) + next_at + place(i));
+                else *reinterpret_cast<u32x4 *>(lds + next_at + place(i) + 16 * lane) = u32x4{0, 0, 0, 0};
+            }
         }
+        next_a += 128 * WK;
+        next_w += T::WB * WK;
+        next_step += 1;
+        next_at = next_at == (S - 1) * T::STAGE ? 0 : next_at + T::STAGE;
     };
+    const uint32_t whole_steps = ends_inside ? steps - 1 : steps;
 
     // Scales, GB bytes of a row at a time.  Where that is four steps and more, a thread loads a row's into registers in the group
     // before and stores them at the barrier before the group; the compiler then waits for the copies under way as well, which costs less
-    // than the instructions of the other way (8192^3, E4M3: 438 against 477 us).  Where it is fewer, copies bring the aligned
+    // than the instructions of the other way (8192^3, E4M3: 430 against 470 us).  Where it is fewer, copies bring the aligned
     // words that hold them (a row begins at any byte; reads are of bytes).  Bytes beyond a row are 2^0 (they meet zeros).
-    auto scale_row = [&](uint32_t q) -> const uint8_t * {              // of activations, then of weights
-        if (T::BYTES && q < (uint32_t)BM) return p.SA + (uint64_t)(m0 + q < p.m ? m0 + q : p.m - 1) * row_scales;
-        const uint32_t n = n0 + q - (T::BYTES ? BM : 0);
-        return p.SW + (uint64_t)(n < p.n ? n : p.n - 1) * row_scales;
-    };
     constexpr uint32_t ONES = SF == MMAEMU_SCALE_FORMAT_UE4M3 ? 0x38383838u : 0x7F7F7F7Fu;
-    constexpr int REGS = T::IN_REGISTERS ? (T::SCALE_ROWS + T::THREADS - 1) / T::THREADS : 1;
-    Words4<1> sreg[REGS];
-    auto load_scales = [&](uint32_t group) {
+    constexpr int REGS = T::IN_REGISTERS ? (T::SCALE_ROWS + T::THREADS - 1) / T::THREADS : (T::WORDS + T::THREADS - 1) / T::THREADS;
+    // rows or words of this thread: their rows' beginnings, and where their next group begins (words: at the aligned word that
+    // holds its first byte)
+    const uint8_t *sbegin[REGS], *sfrom[REGS];
+#pragma unroll
+    for (int i = 0; i < REGS; ++i) {
+        const uint32_t q = i * T::THREADS + tid, all = T::IN_REGISTERS ? T::SCALE_ROWS : T::WORDS, c = q < all ? q : 0;
+        const uint32_t srow = T::IN_REGISTERS ? c : c / T::WPR, row_n = srow - (T::BYTES ? BM : 0);      // of activations, then of weights
+        sbegin[i] = p.SW + (uint64_t)(n0 + (row_n < rows_n ? row_n : rows_n - 1)) * row_scales;
+        if constexpr (T::BYTES) {
+            const uint8_t *of_a = p.SA + (uint64_t)(m0 + (srow < rows_m ? srow : rows_m - 1)) * row_scales;
+            sbegin[i] = srow < (uint32_t)BM ? of_a : sbegin[i];
+        }
+        sfrom[i] = sbegin[i];
+        if (!T::IN_REGISTERS) sfrom[i] += 4 * (c % T::WPR) - ((uintptr_t)sfrom[i] & 3);
+    }
+    uint32_t next_group = 0;                       // the group that sfrom points at
+    Words4<1> sreg[T::IN_REGISTERS ? REGS : 1];
+    uint32_t wreg[T::IN_REGISTERS ? 1 : REGS];
+    auto load_scales = [&]() MMAEMU_INLINE {                     // the next group into registers, byte by byte where a word is not all of its row
 #pragma unroll
         for (int i = 0; i < REGS; ++i) {
-            const uint32_t q = i * T::THREADS + tid;
-            const uint8_t *from = scale_row(q < (uint32_t)T::SCALE_ROWS ? q : 0) + 16 * group;
-            if (16 * group + 16 <= row_scales) sreg[i] = *reinterpret_cast<const Words4<1> *>(from);
-            else {
+            if constexpr (T::IN_REGISTERS) {
+                if (16 * next_group + 16 <= row_scales) sreg[i] = *reinterpret_cast<const Words4<1> *>(sfrom[i]);
+                else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sreg[i].w[e] = ONES;
+                    for (int e = 0; e < 4; ++e) sreg[i].w[e] = ONES;
 #pragma unroll
-                for (uint32_t e = 0; e < 15; ++e)
-                    if (16 * group + e < row_scales) sreg[i].w[e / 4] = (sreg[i].w[e / 4] & ~(0xFFu << (8 * (e % 4)))) | (uint32_t)from[e] << (8 * (e % 4));
-            }
-        }
-    };
-    auto word_of = [&](uint32_t q, uint32_t group) -> const uint8_t * {
-        const uint8_t *from = scale_row(q / T::WPR) + T::GB * group;
-        return from - ((uintptr_t)from & 3) + 4 * (q % T::WPR);
-    };
-    auto put_scales = [&](uint32_t group) {
-        uint8_t *to = scales + (group & 1) * T::SCALES;
-        if constexpr (T::IN_REGISTERS) {
-#pragma unroll
-            for (int i = 0; i < REGS; ++i) {
-                const uint32_t q = i * T::THREADS + tid;
-                if (T::SCALE_ROWS % T::THREADS == 0 || q < (uint32_t)T::SCALE_ROWS) *reinterpret_cast<u32x4 *>(to + 16 * q) = u32x4{sreg[i].w[0], sreg[i].w[1], sreg[i].w[2], sreg[i].w[3]};
-            }
-        } else {
-            for (uint32_t q = tid; q < (uint32_t)T::WORDS; q += T::THREADS) {
-                const uint8_t *begin = scale_row(q / T::WPR), *end = begin + row_scales, *from = word_of(q, group);
-                uint32_t w = ONES;
-                if (from >= begin && from + 4 <= end) w = *reinterpret_cast<const uint32_t *>(from);
+                    for (uint32_t e = 0; e < 15; ++e)
+                        if (16 * next_group + e < row_scales) sreg[i].w[e / 4] = (sreg[i].w[e / 4] & ~(0xFFu << (8 * (e % 4)))) | (uint32_t)sfrom[i][e] << (8 * (e % 4));
+                }
+            } else {
+                const uint8_t *begin = sbegin[i], *end = begin + row_scales, *from = sfrom[i];
+                wreg[i] = ONES;
+                if (from >= begin && from + 4 <= end) wreg[i] = *reinterpret_cast<const uint32_t *>(from);
                 else
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (from + e >= begin && from + e < end) w = (w & ~(0xFFu << (8 * e))) | (uint32_t)from[e] << (8 * e);
-                *reinterpret_cast<uint32_t *>(to + 4 * q) = w;
+                        if (from + e >= begin && from + e < end) wreg[i] = (wreg[i] & ~(0xFFu << (8 * e))) | (uint32_t)from[e] << (8 * e);
             }
+        }
+#pragma unroll
+        for (int i = 0; i < REGS; ++i) sfrom[i] += T::GB;
+        next_group += 1;
+    };
+    auto put_scales = [&](uint32_t half) MMAEMU_INLINE {         // what load_scales has loaded
+#pragma unroll
+        for (int i = 0; i < REGS; ++i) {
+            const uint32_t q = i * T::THREADS + tid;
+            if constexpr (T::IN_REGISTERS) {
+                if (T::SCALE_ROWS % T::THREADS == 0 || q < (uint32_t)T::SCALE_ROWS) *reinterpret_cast<u32x4 *>(scales + half + 16 * q) = u32x4{sreg[i].w[0], sreg[i].w[1], sreg[i].w[2], sreg[i].w[3]};
+            } else if (T::WORDS % T::THREADS == 0 || q < (uint32_t)T::WORDS) *reinterpret_cast<uint32_t *>(scales + half + 4 * q) = wreg[i];
         }
     };
     // copies do it where all words lie within their rows (with rows of aligned words the last is not needed)
     const bool words = row_scales % 4 == 0 && ((uintptr_t)p.SW & 3) == 0 && (!T::BYTES || ((uintptr_t)p.SA & 3) == 0);
-    auto copies_do = [&](uint32_t group) { return !T::IN_REGISTERS && T::GB * group + (words ? T::GB : T::GB + 4) <= row_scales; };
-    auto copy_scales = [&](uint32_t group) {
-        const uint32_t to = lds_address(scales) + (group & 1) * T::SCALES;
-        for (uint32_t q0 = 64 * wave; q0 < (uint32_t)T::WORDS; q0 += T::THREADS) {
-            const uint32_t q = q0 + lane;
-            const uint8_t *from = word_of(q < (uint32_t)T::WORDS ? q : 0, group);
-            if (q < (uint32_t)T::WORDS && !(words && q % T::WPR == T::WPR - 1)) copy_word_to_lds(from, to + 4 * q0);
+    const uint32_t reach = words ? T::GB : T::GB + 4, copied_groups = T::IN_REGISTERS || row_scales < reach ? 0 : (row_scales - reach) / T::GB + 1;
+    auto copy_scales = [&](uint32_t half) MMAEMU_INLINE {
+#pragma unroll
+        for (int i = 0; i < REGS; ++i) {
+            const uint32_t q = i * T::THREADS + tid;
+            if ((T::WORDS % T::THREADS == 0 || q < (uint32_t)T::WORDS) && !(words && q % T::WPR == T::WPR - 1)) copy_word_to_lds(sfrom[i], lds_address(scales) + half + 4 * (i * T::THREADS + 64 * wave));
+            sfrom[i] += T::GB;
         }
+        next_group += 1;
     };
-    const uint32_t row_shift_a = T::BYTES ? (uint32_t)((uintptr_t)p.SA & 3) : 0u, row_shift_w = (uint32_t)((uintptr_t)p.SW & 3);
 
     constexpr int MT = TM / 16, NT = TN / 16;
     const uint32_t block = wave % T::BLOCKS, kw = wave / T::BLOCKS, wm = (block % T::BLOCKS_M) * TM, wn = (block / T::BLOCKS_M) * TN;
@@ -145,20 +169,11 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc[j][i] = f32x4{0, 0, 0, 0};
 
-    // byte of a row's first staged scale: its words, and where in them the row's bytes begin
-    uint32_t at_w[NT], at_a[T::BYTES ? MT : 1];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const uint32_t row = wn + 16 * j + r, n = n0 + row < p.n ? n0 + row : p.n - 1;
-        at_w[j] = ((T::BYTES ? BM : 0) + row) * (4 * T::WPR) + (T::IN_REGISTERS ? 0u : (row_shift_w + n * row_scales) & 3) + (T::BYTES ? g : SF == MMAEMU_SCALE_FORMAT_E8M0 ? g / 2 : g);
-    }
-    if constexpr (T::BYTES) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const uint32_t row = wm + 16 * i + r, m = m0 + row < p.m ? m0 + row : p.m - 1;
-            at_a[i] = row * (4 * T::WPR) + (T::IN_REGISTERS ? 0u : (row_shift_a + m * row_scales) & 3) + g;
-        }
-    }
+    // byte of a row's first staged scale: its words, and where in them the row's bytes begin (the same for rows 16 apart)
+    const uint32_t row_w = wn + r, row_a = wm + r;
+    const uint32_t at_w = ((T::BYTES ? BM : 0) + row_w) * (4 * T::WPR) + (T::IN_REGISTERS ? 0u : ((uint32_t)(uintptr_t)p.SW + (n0 + row_w) * row_scales) & 3) +
+                          kw * T::SB + (T::BYTES ? g : SF == MMAEMU_SCALE_FORMAT_E8M0 ? g / 2 : g);
+    const uint32_t at_a = T::BYTES ? row_a * (4 * T::WPR) + (T::IN_REGISTERS ? 0u : ((uint32_t)(uintptr_t)p.SA + (m0 + row_a) * row_scales) & 3) + kw * T::SB + g : 0u;
 
     // What a wavefront holds of its part of a step: weights as they are stored, their scales, and activations.
     struct Part {
@@ -166,25 +181,24 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
         u32x2 c[T::BYTES ? 1 : NT];
         uint32_t ws[NT], xs[T::BYTES ? MT : 1];
     };
-    auto read_part = [&](Part &q, uint32_t s) {
-        const uint8_t *a = lds + (s % S) * T::STAGE + kw * T::A_PART + (wm + r) * 128, *w = lds + (s % S) * T::STAGE + T::A_BYTES + kw * T::W_PART + (wn + r) * T::WB;
-        const uint8_t *sc = scales + ((s / T::GROUP) & 1) * T::SCALES + (s % T::GROUP * WK + kw) * T::SB;
-        w += T::BYTES ? 16 * (g ^ (r >> 2)) : 8 * g;
+    const uint32_t in_a = kw * T::A_PART + (wm + r) * 128, in_w = T::A_BYTES + kw * T::W_PART + (wn + r) * T::WB + (T::BYTES ? 16 * (g ^ (r >> 2)) : 8 * g);
+    const uint32_t in_lo = in_a + 16 * ((T::BYTES ? g : 2 * g) ^ rot), in_hi = in_a + 16 * ((T::BYTES ? 4 + g : 2 * g + 1) ^ rot);
+    auto read_part = [&](Part &q, uint32_t at, uint32_t sc) MMAEMU_INLINE {          // of the step in the buffer `at`, its scales at sc
+        const uint8_t *w = lds + at + in_w, *lo = lds + at + in_lo, *hi = lds + at + in_hi, *sw = scales + sc + at_w, *sa = scales + sc + at_a;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             if constexpr (T::BYTES) q.wf[j] = *reinterpret_cast<const u32x4 *>(w + 16 * T::WB * j);
             else q.c[j] = *reinterpret_cast<const u32x2 *>(w + 16 * T::WB * j);
-            q.ws[j] = sc[at_w[j]];
+            q.ws[j] = sw[64 * T::WPR * j];
         }
-        const uint8_t *lo = a + 16 * ((T::BYTES ? g : 2 * g) ^ rot), *hi = a + 16 * ((T::BYTES ? 4 + g : 2 * g + 1) ^ rot);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             q.x[i][0] = *reinterpret_cast<const u32x4 *>(lo + 2048 * i);
             q.x[i][1] = *reinterpret_cast<const u32x4 *>(hi + 2048 * i);
-            if constexpr (T::BYTES) q.xs[i] = sc[at_a[i]];
+            if constexpr (T::BYTES) q.xs[i] = sa[64 * T::WPR * i];
         }
     };
-    auto multiply = [&](const Part &q) {
+    auto multiply = [&](const Part &q) MMAEMU_INLINE {
         if constexpr (T::BYTES) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
@@ -237,66 +251,83 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
         }
     };
 
-    static_assert(T::IN_REGISTERS || T::GROUP >= S - 2, "scales come in time");
-    // Before step s is read: its copies have come, in all wavefronts; those of the S - 2 steps after it may be under way.  A group's
-    // scales are copied in the group before, at least S - 2 steps ahead, so that this wait covers them.
-    auto arrive = [&](uint32_t s) {
-        if (s % T::GROUP == 0 && s && !copies_do(s / T::GROUP)) put_scales(s / T::GROUP);       // (into the half that was read a group ago)
-        const uint32_t after = s + 1 < full ? full - 1 - s : 0;
-        if (after >= S - 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S - 2) * T::COPIES) : "memory");
-        else if (S > 3 && after >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * T::COPIES) : "memory");
-        else if (S > 3 && after == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(T::COPIES) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (s == full) {                                               // the step that ends inside: products beyond the row are zero times zero
-#pragma unroll
-            for (int i = 0; i < T::COPIES; ++i) {
-                u32x4 v = {0, 0, 0, 0};
-                if (s * T::KS + product_of(i) < p.k) v = *reinterpret_cast<const u32x4 *>(src[i] + (uint64_t)s * (i < T::AC ? 128 * WK : T::WB * WK));
-                *reinterpret_cast<u32x4 *>(lds + (s % S) * T::STAGE + (i < T::AC ? 0 : T::A_BYTES) + 16 * chunk_of(i)) = v;
-            }
-            __syncthreads();
-        }
-        if (s % T::GROUP == 0 && s + T::GROUP < steps) {
-            if constexpr (T::IN_REGISTERS) load_scales(s / T::GROUP + 1);
-            else if (copies_do(s / T::GROUP + 1)) copy_scales(s / T::GROUP + 1);
+    static_assert(S <= 3, "waits for one step or none under way");
+    // The step that is read next: its buffer and its place among the scales.
+    uint32_t at = 0, in_group = 0, half = 0;
+    auto go_on = [&]() MMAEMU_INLINE {
+        at = at == (S - 1) * T::STAGE ? 0 : at + T::STAGE;
+        if (++in_group == T::GROUP) {
+            in_group = 0;
+            half ^= T::SCALES;
         }
     };
-    if constexpr (T::IN_REGISTERS) load_scales(0);
+    // Before step s is read: its copies have come, in all wavefronts; those of the S - 2 steps after it may be under way.  A group's
+    // scales are copied in the group before, at least S - 2 steps ahead, so that this wait covers them.  (STEADY: away from the
+    // end, where nothing has to be asked.)
+    auto arrive = [&](uint32_t s, auto steady) MMAEMU_INLINE {
+        if constexpr (steady && !T::IN_REGISTERS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S - 2) * T::COPIES) : "memory");
+        else {
+            if (in_group == 0 && s && s / T::GROUP >= copied_groups) put_scales(half);         // (into the half that was read a group ago)
+            // (a step that ends inside counts as none: it may have fewer copies)
+            if (S == 3 && (steady || s + 1 < whole_steps)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S - 2) * T::COPIES) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        }
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (in_group == 0 && (steady || s + T::GROUP < steps)) {
+            if (!T::IN_REGISTERS && (steady || s / T::GROUP + 1 < copied_groups)) copy_scales(half ^ T::SCALES);
+            else load_scales();
+        }
+    };
+    // steps before which all that is waited for or issued is whole
+    constexpr uint32_t AHEAD = PIPE ? S : S - 1;   // steps issued ahead of the one that is multiplied
+    uint32_t steady_steps = whole_steps > AHEAD ? whole_steps - AHEAD : 0;
+    if (!T::IN_REGISTERS) {
+        const uint32_t last = copied_groups > 1 ? (copied_groups - 1) * T::GROUP : 0;
+        if (last < steady_steps + (PIPE ? 1 : 0)) steady_steps = PIPE ? (last ? last - 1 : 0) : last;
+    } else if (steady_steps * T::SB * WK + 32 > row_scales) steady_steps = row_scales >= 32 ? (row_scales - 32) / (T::SB * WK) : 0;
+    load_scales();
+#pragma unroll
+    for (uint32_t s = 0; s < AHEAD; ++s)
+        if (s < steps) issue(s < whole_steps);
     put_scales(0);
+    uint32_t s = 0;
     if constexpr (PIPE) {
         // The part of step s + 1 is read into registers before the products of step s, whose buffer then takes the copies of
         // step s + S.
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-            if (s < (int)full) issue(s);
         Part one, two;
-        arrive(0);                                                     // (waits for one step more than it has to)
-        read_part(one, 0);
-        auto step = [&](uint32_t s, const Part &now, Part &next) {
-            if (s + 1 < steps) {
-                arrive(s + 1);
-                read_part(next, s + 1);
-                if (s + S < full) issue(s + S);
+        arrive(0, std::false_type());                                  // (waits for one step more than it has to)
+        read_part(one, at, half + in_group * (WK * T::SB));
+        auto step = [&](const Part &now, Part &next, auto steady) MMAEMU_INLINE {
+            if (steady || s + 1 < steps) {
+                go_on();
+                arrive(s + 1, steady);
+                read_part(next, at, half + in_group * (WK * T::SB));
+                if (steady || s + S < steps) issue(steady || s + S < whole_steps);
             }
             multiply(now);
+            ++s;
         };
-        for (uint32_t s = 0; s < steps; s += 2) {
-            step(s, one, two);
-            if (s + 1 < steps) step(s + 1, two, one);
+        while (s + 1 < steady_steps) {
+            step(one, two, std::true_type());
+            step(two, one, std::true_type());
+        }
+        while (s < steps) {
+            step(one, two, std::false_type());
+            if (s < steps) step(two, one, std::false_type());
         }
     } else {
-#pragma unroll
-        for (int s = 0; s < S - 1; ++s)
-            if (s < (int)full) issue(s);
-        for (uint32_t s = 0; s < steps; ++s) {
-            arrive(s);
-            if (s + S - 1 < full) issue(s + S - 1);                    // into the buffer that all have left
+        auto step = [&](auto steady) MMAEMU_INLINE {
+            arrive(s, steady);
+            if (steady || s + S - 1 < steps) issue(steady || s + S - 1 < whole_steps);          // into the buffer that all have left
             Part q;
-            read_part(q, s);
+            read_part(q, at, half + in_group * (WK * T::SB));
+            go_on();
             multiply(q);
-        }
+            ++s;
+        };
+        while (s < steady_steps) step(std::true_type());
+        while (s < steps) step(std::false_type());
     }
     if constexpr (WK > 1) {                                            // the sums of the wavefronts that share a block
         __syncthreads();
@@ -333,17 +364,17 @@ template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S, bool PI
     return MMAEMU_OK;
 }
 
-// Which block: the one whose rounds of workgroups over the 256 compute units take least, by what a round of each took (us for
-// 8192 products, 8- and 16-bit activations, with all units at work).  A larger block reads less per product, a smaller one
-// fills the chip with fewer rows; both sides were measured at the places where the choice changes, E4M3 and BF16 activations
-// on MXFP4 weights, times in us:
-//   m = 2048, n = 8192, k = 4096: 256 x 256 70 and 124, 128 x 256 79 and 148;   m = 256, n = 28672, k = 8192: 128 x 256 77 and 144, 256 x 256 121 and 223
-//   m = 512, n = 8192, k = 8192: 128 x 128 45 and 72, 64 x 64 76 and 113;       m = 128, n = 8192, k = 8192: 64 x 64 21 and 31, 32 x 64 25 and 31
-//   m = 64, n = 8192, k = 8192: 32 x 64 15 and 22, 64 x 64 20 and 29;           m = 32, n = 8192, k = 8192: 32 x 32 11 and 14, 32 x 64 14 and 22
-struct BlockChoice { uint32_t bm, bn; float one[2], two[2]; };         // two: of 512 workgroups (two of the 32 x 64 ones fit a unit)
+// Which block: the one whose rounds of workgroups over the 256 compute units take least, by what one round and two rounds took (us
+// for 8192 products, E4M3 and BF16 activations on MXFP4 weights; of some blocks two workgroups fit a unit).  A larger block reads
+// less per product, a smaller one fills the chip with fewer tokens and splits its products among more wavefronts.  Both sides
+// where the choice changes, E4M3 and BF16, us:
+//   2048 tokens, 8192 x 4096: 256 x 256 62 and 115, 128 x 256 70 and 132;  256 tokens, 28672 x 8192: 128 x 256 68 and 127, 256 x 256 103 and 215
+//   512 tokens, 8192 x 8192: 128 x 128 37 and 67, 64 x 128 41 and 76;      256 tokens: 64 x 128 25 and 46, 64 x 64 27 (E4M3), 32 x 64 53 (BF16), 128 x 128 35 and 66
+//   128 tokens: 64 x 64 18 (E4M3), 32 x 64 23 and 28, 64 x 128 23 and 46;  64 tokens: 32 x 64 13 and 19, 64 x 64 17 (E4M3), 32 x 32 17 and 23;  32 tokens: 32 x 32 11 and 13, 32 x 64 13 and 19
+struct BlockChoice { uint32_t bm, bn; float one[2], two[2]; };                // (0: not built for 16-bit activations, where 32 x 64 or 64 x 128 takes less anywhere)
 static const BlockChoice BLOCK_CHOICES[] = {
-    {256, 256, {119, 223}, {238, 446}}, {128, 256, {72, 139}, {144, 278}}, {128, 128, {45, 72}, {90, 144}},
-    {64, 64, {21, 30}, {42, 60}},       {32, 64, {14.5f, 22}, {26, 31}},   {32, 32, {11, 14}, {22, 28}},
+    {256, 256, {112, 225}, {224, 450}}, {128, 256, {65, 126}, {130, 252}}, {128, 128, {37, 67}, {74, 134}}, {64, 128, {24.6f, 46}, {48, 76}},
+    {64, 64, {17.6f, 0}, {27.4f, 0}}, {32, 64, {13.4f, 19.3f}, {23, 27.8f}}, {32, 32, {11, 13.3f}, {17, 23.4f}},
 };
 
 static uint32_t choose_block(uint32_t m, uint32_t n, bool bytes, bool fp16_e8m0)
@@ -352,6 +383,7 @@ static uint32_t choose_block(uint32_t m, uint32_t n, bool bytes, bool fp16_e8m0)
     float least = 0;
     for (uint32_t i = fp16_e8m0 ? 1 : 0; i < sizeof(BLOCK_CHOICES) / sizeof(BLOCK_CHOICES[0]); ++i) {      // (FP16 activations' second way leaves too few registers for 256 x 256)
         const BlockChoice &b = BLOCK_CHOICES[i];
+        if (b.one[bytes ? 0 : 1] == 0) continue;
         const uint64_t tiles = (uint64_t)((m + b.bm - 1) / b.bm) * ((n + b.bn - 1) / b.bn);
         const uint64_t rounds = (tiles + 255) / 256;
         const float t = b.two[bytes ? 0 : 1] * (float)(rounds / 2) + (rounds % 2 ? b.one[bytes ? 0 : 1] : 0.0f);
@@ -365,7 +397,7 @@ static uint32_t choose_block(uint32_t m, uint32_t n, bool bytes, bool fp16_e8m0)
 
 const char *tiled_name(uint32_t m, uint32_t n, uint32_t a_type, uint32_t scale_format)
 {
-    static const char *const names[] = {"blocks of 256 x 256", "blocks of 128 x 256", "blocks of 128 x 128", "blocks of 64 x 64", "blocks of 32 x 64", "blocks of 32 x 32"};
+    static const char *const names[] = {"blocks of 256 x 256", "blocks of 128 x 256", "blocks of 128 x 128", "blocks of 64 x 128", "blocks of 64 x 64", "blocks of 32 x 64", "blocks of 32 x 32"};
     return names[choose_block(m, n, is_byte_type(a_type), a_type == MMAEMU_FP16 && scale_format == MMAEMU_SCALE_FORMAT_E8M0)];
 }
 
@@ -373,17 +405,17 @@ template <int AT, int SF> static mmaemu_status launch_tiled_typed(const ProductA
 {
     constexpr bool BYTES = AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2, TWO_WAYS = AT == MMAEMU_FP16 && SF == MMAEMU_SCALE_FORMAT_E8M0;
     switch (choose_block(p.m, p.n, BYTES, TWO_WAYS)) {
+    // (the wavefront's share, the depth of the buffers and the reading ahead: what was fastest for each kind of activations; wavefronts that
+    // take weights to 16 bits have fewer of them and more tokens: 2048 x 8192 x 4096 under UE4M3 scales 191 -> 144 us)
     case 0:
-        // (BF16 weights under UE4M3 scales take four instructions a pair: blocks of fewer weights per wavefront, 200 -> 157 us at
-        // 2048 x 8192 x 4096)
-        if constexpr (AT == MMAEMU_BF16 && SF == MMAEMU_SCALE_FORMAT_UE4M3) return launch_tile<AT, SF, 256, 256, 128, 64, 1, 3, false>(p, s);
-        else if constexpr (!TWO_WAYS) return launch_tile<AT, SF, 256, 256, 64, 128, 1, 3, false>(p, s);
-    case 1: return launch_tile<AT, SF, 128, 256, 64, 64, 1, 3, !TWO_WAYS>(p, s);
-    case 2: return launch_tile<AT, SF, 128, 128, 64, 64, 2, 2, !TWO_WAYS>(p, s);
-    case 3:
-        if constexpr (BYTES) return launch_tile<AT, SF, 64, 64, 32, 32, 4, 2, false>(p, s);
-        else return launch_tile<AT, SF, 64, 64, 64, 32, 4, 2, false>(p, s);
-    case 4: return launch_tile<AT, SF, 32, 64, 32, 32, 4, 3, false>(p, s);
+        if constexpr (BYTES) return launch_tile<AT, SF, 256, 256, 64, 128, 1, 3, false>(p, s);
+        else if constexpr (!TWO_WAYS) return launch_tile<AT, SF, 256, 256, 128, 64, 1, 3, false>(p, s);
+    case 1: return launch_tile<AT, SF, 128, 256, 64, 64, 1, 3, !BYTES && !TWO_WAYS>(p, s);
+    case 2: return launch_tile<AT, SF, 128, 128, 64, 64, 2, 3, !BYTES && !TWO_WAYS>(p, s);
+    case 3: return launch_tile<AT, SF, 64, 128, 64, 32, 2, BYTES ? 3 : 2, false>(p, s);
+    case 4:
+        if constexpr (BYTES) return launch_tile<AT, SF, 64, 64, 32, 32, 2, 3, false>(p, s);
+    case 5: return launch_tile<AT, SF, 32, 64, 32, 32, 4, 3, false>(p, s);
     default: return launch_tile<AT, SF, 32, 32, 32, 32, 8, 3, false>(p, s);
     }
 }

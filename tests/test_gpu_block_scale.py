@@ -415,8 +415,9 @@ def test_chain_on_a_stream_and_in_a_graph():
         assert (np.abs(got - av @ wv.T) <= product_bound(av, wv, mm.E4M3) + np.abs(av @ wv.T) * 2.0 ** -23).all()
 
 
+SIXTEEN = {mm.BF16: True, mm.FP16: True, mm.E4M3: False, mm.E5M2: False}
 KERNELS = [("stream", 1, 30), ("stream", 4, 4097), ("stream", 5, 100), ("stream", 8, 16401), ("stream", 9, 70), ("stream", 16, 4110), ("stream", 13, 16390),
-           ("blocks of 32 x 32", 17, 40), ("blocks of 32 x 64", 77, 5003), ("blocks of 64 x 64", 250, 4093), ("blocks of 128 x 128", 500, 8190),
+           ("blocks of 32 x 32", 17, 40), ("blocks of 32 x 64", 77, 5003), ("blocks of 64 x 64", 250, 4093), ("blocks of 64 x 128", 250, 8190), ("blocks of 128 x 128", 500, 8190),
            ("blocks of 128 x 256", 250, 28000), ("blocks of 256 x 256", 4090, 4085)]
 
 
@@ -425,7 +426,8 @@ KERNELS = [("stream", 1, 30), ("stream", 4, 4097), ("stream", 5, 100), ("stream"
 def test_product_every_kernel(name, m, n, at, fmt):
     """Every kernel, at sizes that its blocks do not divide and products that end inside a step, or do not fill one: every output against the
     sum of the magnitudes, and some against the bound of their own products."""
-    if not (name == "blocks of 256 x 256" and at == mm.FP16 and fmt == bs.SCALE_E8M0):
+    # (256 x 256 is not built for FP16 activations on MXFP4 weights, 64 x 64 not for 16-bit ones)
+    if not (name == "blocks of 256 x 256" and at == mm.FP16 and fmt == bs.SCALE_E8M0) and not (name == "blocks of 64 x 64" and SIXTEEN[at]):
         assert mm.matmul_fp4_kernel(m, n, 32, at, fmt) == name
     rng = np.random.default_rng(m + n)
     for k in (32, 416, 1024, 2144):

@@ -123,6 +123,18 @@ __device__ __forceinline__ void copy_word_to_lds(const uint8_t *from, uint32_t t
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
 }
 
+// Reads of sixteen bytes per lane serve the lanes 0 - 3, 12 - 15, 20 - 27 together, then 4 - 11, 16 - 19, 28 - 31, and so the upper 32; the
+// sixteen have to differ in their place within 256 bytes (found with the conflict counter).  Lane l reads row l % 16, and its group of
+// lanes l / 16 picks the 16-byte chunk: chunk c of row r is stored at c ^ lds_rotation<chunks of a row>(r).
+template <int CHUNKS> __device__ __forceinline__ constexpr uint32_t lds_rotation(uint32_t r)
+{
+    const uint32_t r1 = (r >> 1) & 1, r2 = (r >> 2) & 1, r3 = (r >> 3) & 1;
+    if (CHUNKS == 16) return (r2 ^ r3) << 3 | r3 << 2 | (r & 3);
+    if (CHUNKS == 8) return (r2 ^ r3) << 2 | r3 << 1 | r1;
+    if (CHUNKS == 4) return (r >> 1) & 3;
+    return r3;                                     // two: 32 bytes, read by eights
+}
+
 struct ProductArgs {
     const uint8_t *A, *SA, *W, *SW;
     void *D;

@@ -18,8 +18,9 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> struct Strea
     static constexpr int W_BYTES = 16 * NT * WROW, X_BYTES = DW * MR * XB, SLOT = W_BYTES + X_BYTES;
     static constexpr int WC = W_BYTES / 1024, XC = (X_BYTES + 1023) / 1024, COPIES = WC + XC;
     static constexpr int RUN = 16;                                     // windows whose scales are staged together
-    static constexpr int SW_ROW = RUN * SB, SX_ROW = RUN * 4;          // bytes of a row's scales in a run
-    static constexpr int SW_BYTES = 16 * NT * SW_ROW, SX_BYTES = BYTES ? MR * SX_ROW : 0;
+    static constexpr int SW_ROW = RUN * SB, SX_ROW = RUN * 4;          // bytes of a row's scales in a run,
+    static constexpr int SW_PITCH = SW_ROW + 16, SX_PITCH = SX_ROW + 16;               // and what rows are apart: no two in a bank
+    static constexpr int SW_BYTES = 16 * NT * SW_PITCH, SX_BYTES = BYTES ? MR * SX_PITCH : 0;
     static constexpr int WAVE_LDS = R * SLOT + SW_BYTES + SX_BYTES;
     static constexpr int SUM_LDS = NT * WAVES * 1024;
     static constexpr int LDS = WAVES * WAVE_LDS > SUM_LDS ? WAVES * WAVE_LDS : SUM_LDS;
@@ -70,15 +71,14 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
     const uint32_t slots = (p.k + 128 * DW - 1) / (128 * DW), per = slots / WAVES, more = slots % WAVES;
     const uint32_t first = wave * per + (wave < more ? wave : more), count = per + (wave < more ? 1 : 0);
 
-    // Sources of this lane's copies.  Rows of 128 bytes and more are stored with their 16-byte chunks rotated, so that the lanes
-    // that read together find them in different banks.
+    // sources of this lane's copies, chunks stored where lds_rotation puts them
     const uint8_t *src[T::COPIES];
     uint32_t src_k[T::COPIES];                     // products before the chunk, within the slot
     bool src_in[T::COPIES];
 #pragma unroll
     for (int i = 0; i < T::WC; ++i) {
         const uint32_t chunk = 64 * i + lane, row = chunk / (4 * DW), pos = chunk % (4 * DW);
-        const uint32_t c = DW == 2 ? pos ^ ((row >> 1) & 7) : pos ^ ((row >> 2) & 3);
+        const uint32_t c = pos ^ lds_rotation<4 * DW>(row);
         const uint32_t n = n0 + row < p.n ? n0 + row : p.n - 1;
         src[i] = p.W + (uint64_t)n * (p.k / 2) + (uint64_t)first * T::WROW + 16 * c;
         src_k[i] = 32 * c;
@@ -88,7 +88,7 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
     for (int i = 0; i < T::XC; ++i) {
         constexpr uint32_t PER_ROW = T::XB / 16;
         const uint32_t chunk = 64 * i + lane, win = chunk / (MR * PER_ROW), row = chunk / PER_ROW % MR, pos = chunk % PER_ROW;
-        const uint32_t c = pos ^ (T::BYTES ? (row >> 1) & 7 : row & 15);
+        const uint32_t c = pos ^ lds_rotation<T::XB / 16>(row);
         const uint32_t m = row;
         src_in[T::WC + i] = chunk < (uint32_t)T::X_BYTES / 16;          // (tokens that are not there: the last one again)
         src[T::WC + i] = p.A + (uint64_t)(m < p.m ? m : p.m - 1) * p.a_stride + (uint64_t)first * (DW * T::XB) + win * T::XB + 16 * c;
@@ -113,14 +113,14 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
     };
     // scales of sixteen windows from this wavefront's slot d on: sixteen bytes per lane, byte by byte at a row's end
     auto stage_scales = [&](uint32_t d) MMAEMU_INLINE {
-        constexpr uint32_t PIECES = (16 * NT * T::SW_ROW + T::SX_BYTES) / 16;
+        constexpr uint32_t W_PIECES = 16 * NT * T::SW_ROW / 16, PIECES = W_PIECES + (T::BYTES ? MR * T::SX_ROW / 16 : 0);
         const uint32_t w0 = (first + d) * DW;      // first window
 #pragma unroll
         for (uint32_t q0 = 0; q0 < PIECES; q0 += 64) {
             const uint32_t q = q0 + lane;
             if (PIECES % 64 && q >= PIECES) break;
-            const bool of_w = q < (uint32_t)T::SW_BYTES / 16;
-            const uint32_t x = q - T::SW_BYTES / 16, row = of_w ? q / (T::SW_ROW / 16) : x / (T::SX_ROW / 16), at = 16 * (of_w ? q % (T::SW_ROW / 16) : x % (T::SX_ROW / 16));
+            const bool of_w = q < W_PIECES;
+            const uint32_t x = q - W_PIECES, row = of_w ? q / (T::SW_ROW / 16) : x / (T::SX_ROW / 16), at = 16 * (of_w ? q % (T::SW_ROW / 16) : x % (T::SX_ROW / 16));
             const uint32_t n = n0 + row < p.n ? n0 + row : p.n - 1, m = row < p.m ? row : p.m - 1;
             const uint32_t all = of_w ? p.k / (128 / T::SB) : p.k / 32, begin = w0 * (of_w ? T::SB : 4) + at;
             const uint8_t *from = (of_w ? p.SW + (uint64_t)n * all : p.SA + (uint64_t)m * all) + begin;
@@ -133,7 +133,7 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
                 for (uint32_t e = 0; e < 15; ++e)
                     if (begin + e < all) v.w[e / 4] = (v.w[e / 4] & ~(0xFFu << (8 * (e % 4)))) | (uint32_t)from[e] << (8 * (e % 4));
             }
-            *reinterpret_cast<u32x4 *>((of_w ? sw_lds : sx_lds - T::SW_BYTES) + 16 * q) = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+            *reinterpret_cast<u32x4 *>((of_w ? sw_lds + row * T::SW_PITCH : sx_lds + row * T::SX_PITCH) + at) = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
         }
     };
 
@@ -159,20 +159,20 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
             uint32_t sx = 0;
             if constexpr (T::BYTES) {
                 const uint8_t *row = xs + (h * MR + rx) * 128;
-                const uint32_t rot = (rx >> 1) & 7;
+                const uint32_t rot = lds_rotation<8>(rx);
                 x[0] = *reinterpret_cast<const u32x4 *>(row + 16 * (g ^ rot));
                 x[1] = *reinterpret_cast<const u32x4 *>(row + 16 * ((4 + g) ^ rot));
-                sx = sx_lds[rx * T::SX_ROW + 4 * win + g];
+                sx = sx_lds[rx * T::SX_PITCH + 4 * win + g];
             } else {
                 const uint8_t *row = xs + (h * MR + rx) * 256;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const u32x4 *>(row + 16 * ((4 * g + j) ^ rx));
+                for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const u32x4 *>(row + 16 * ((4 * g + j) ^ lds_rotation<16>(rx)));
             }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const uint32_t c = DW == 2 ? (4 * h + g) ^ ((r >> 1) & 7) : g ^ (r >> 2);
+                const uint32_t c = (4 * h + g) ^ lds_rotation<4 * DW>(r);
                 const u32x4 w = *reinterpret_cast<const u32x4 *>(slot + (16 * j + r) * T::WROW + 16 * c);
-                const uint8_t *sr = sw_lds + (16 * j + r) * T::SW_ROW + T::SB * win;
+                const uint8_t *sr = sw_lds + (16 * j + r) * T::SW_PITCH + T::SB * win;
                 const uint32_t sc = SF == MMAEMU_SCALE_FORMAT_E8M0 ? sr[g] : *reinterpret_cast<const uint16_t *>(sr + 2 * g);
                 acc[j] = window_products<AT, SF>(w, sc, x, sx, acc[j]);
             }

@@ -44,14 +44,14 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
     const uint32_t steps = (p.k + T::KS - 1) / T::KS, row_scales = p.k / T::PER_SCALE;
     const bool ends_inside = steps * T::KS > p.k;                      // the last step: products beyond the row are zero times zero
 
-    // Source of each of this thread's copies, from the block's first row: part, row, 16-byte chunk of it.  Chunks are stored rotated
-    // by the row, so that the sixteen rows that lanes read together lie in different banks.
+    // Source of each of this thread's copies, from the block's first row: part, row, 16-byte chunk of it.  Chunks are stored where
+    // lds_rotation puts them.
     uint32_t src[T::COPIES];
     auto chunk_of = [&](int i) MMAEMU_INLINE -> uint32_t { return i < T::AC ? (i * T::THREADS + tid) % (T::A_BYTES / 16) : ((i - T::AC) * T::THREADS + tid) % (T::W_BYTES / 16); };
     auto product_of = [&](int i) MMAEMU_INLINE -> uint32_t {                         // the chunk's first product within the step
         const uint32_t q = chunk_of(i);
-        if (i < T::AC) return T::PART * (q / (T::A_PART / 16)) + (T::BYTES ? 16 : 8) * ((q % 8) ^ ((q / 16) & 7));
-        return T::PART * (q / (T::W_PART / 16)) + 32 * (T::BYTES ? (q % 4) ^ ((q / 16) & 3) : q % 2);
+        if (i < T::AC) return T::PART * (q / (T::A_PART / 16)) + (T::BYTES ? 16 : 8) * ((q % 8) ^ lds_rotation<8>(q / 8));
+        return T::PART * (q / (T::W_PART / 16)) + 32 * (T::BYTES ? (q % 4) ^ lds_rotation<4>(q / 4) : (q % 2) ^ lds_rotation<2>(q / 2));
     };
     const uint32_t rows_m = p.m - m0 < BM ? p.m - m0 : BM, rows_n = p.n - n0 < BN ? p.n - n0 : BN;      // (rows beyond: the last one again)
 #pragma unroll
@@ -143,7 +143,12 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
         for (int i = 0; i < REGS; ++i) {
             const uint32_t q = i * T::THREADS + tid;
             if constexpr (T::IN_REGISTERS) {
-                if (T::SCALE_ROWS % T::THREADS == 0 || q < (uint32_t)T::SCALE_ROWS) *reinterpret_cast<u32x4 *>(scales + half + 16 * q) = u32x4{sreg[i].w[0], sreg[i].w[1], sreg[i].w[2], sreg[i].w[3]};
+                if (T::SCALE_ROWS % T::THREADS == 0 || q < (uint32_t)T::SCALE_ROWS) {
+                    // (rows eight apart would meet in a bank: every other eight has its words exchanged in pairs)
+                    const bool swap = (q & 8) != 0;
+                    const uint32_t *w = sreg[i].w;
+                    *reinterpret_cast<u32x4 *>(scales + half + 16 * q) = u32x4{swap ? w[1] : w[0], swap ? w[0] : w[1], swap ? w[3] : w[2], swap ? w[2] : w[3]};
+                }
             } else if (T::WORDS % T::THREADS == 0 || q < (uint32_t)T::WORDS) *reinterpret_cast<uint32_t *>(scales + half + 4 * q) = wreg[i];
         }
     };
@@ -162,7 +167,7 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
 
     constexpr int MT = TM / 16, NT = TN / 16;
     const uint32_t block = wave % T::BLOCKS, kw = wave / T::BLOCKS, wm = (block % T::BLOCKS_M) * TM, wn = (block / T::BLOCKS_M) * TN;
-    const uint32_t rot = (r >> 1) & 7;                                 // (tiles begin at multiples of 16 rows)
+    const uint32_t rot = lds_rotation<8>(r);                                // (tiles begin at multiples of 16 rows)
     f32x4 acc[NT][MT];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -181,9 +186,11 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
         u32x2 c[T::BYTES ? 1 : NT];
         uint32_t ws[NT], xs[T::BYTES ? MT : 1];
     };
-    const uint32_t in_a = kw * T::A_PART + (wm + r) * 128, in_w = T::A_BYTES + kw * T::W_PART + (wn + r) * T::WB + (T::BYTES ? 16 * (g ^ (r >> 2)) : 8 * g);
+    const uint32_t in_a = kw * T::A_PART + (wm + r) * 128, in_w = T::A_BYTES + kw * T::W_PART + (wn + r) * T::WB + (T::BYTES ? 16 * (g ^ lds_rotation<4>(r)) : 16 * ((g >> 1) ^ lds_rotation<2>(r)) + 8 * (g & 1));
     const uint32_t in_lo = in_a + 16 * ((T::BYTES ? g : 2 * g) ^ rot), in_hi = in_a + 16 * ((T::BYTES ? 4 + g : 2 * g + 1) ^ rot);
-    auto read_part = [&](Part &q, uint32_t at, uint32_t sc) MMAEMU_INLINE {          // of the step in the buffer `at`, its scales at sc
+    const uint32_t swapped = T::IN_REGISTERS ? (r & 8) / 2 : 0u;
+    auto read_part = [&](Part &q, uint32_t at, uint32_t half, uint32_t in_group) MMAEMU_INLINE {       // of the step in the buffer `at`, its scales in that half
+        const uint32_t sc = half + ((in_group * (WK * T::SB)) ^ swapped);
         const uint8_t *w = lds + at + in_w, *lo = lds + at + in_lo, *hi = lds + at + in_hi, *sw = scales + sc + at_w, *sa = scales + sc + at_a;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
@@ -297,12 +304,12 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
         // step s + S.
         Part one, two;
         arrive(0, std::false_type());                                  // (waits for one step more than it has to)
-        read_part(one, at, half + in_group * (WK * T::SB));
+        read_part(one, at, half, in_group);
         auto step = [&](const Part &now, Part &next, auto steady) MMAEMU_INLINE {
             if (steady || s + 1 < steps) {
                 go_on();
                 arrive(s + 1, steady);
-                read_part(next, at, half + in_group * (WK * T::SB));
+                read_part(next, at, half, in_group);
                 if (steady || s + S < steps) issue(steady || s + S < whole_steps);
             }
             multiply(now);
@@ -321,7 +328,7 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
             arrive(s, steady);
             if (steady || s + S - 1 < steps) issue(steady || s + S - 1 < whole_steps);          // into the buffer that all have left
             Part q;
-            read_part(q, at, half + in_group * (WK * T::SB));
+            read_part(q, at, half, in_group);
             go_on();
             multiply(q);
             ++s;

@@ -584,7 +584,8 @@ mmaemu_status mmaemu_quantize_fp4(const void *x, void *codes, void *scales, void
  *     binding preset mfma_scale_id(E4M3, E2M1)), so an output may be off by 8 * 2^-13 of the largest product of each eight.
  * d_type: FP32, BF16 or FP16 (nearest even, overflow gives infinities).  Rows of A are a_stride elements apart (0: k), those of
  * D d_stride (0: n).  A NaN scale makes the outputs of its row of A or W NaN.  D may not overlap the inputs.  m = 0 is a
- * no-op.  Forward only; one launch without workspace; the order of a sum depends on m, n, k and types only.
+ * no-op.  Forward only; one launch, or two where whole rounds of blocks and the rest go faster apart, without workspace;
+ * the order of a sum depends on m, n, k and types only.
  * Errors: SHAPE (n or k zero, k not a multiple of 32, k > 2^20, a stride below its row, over 2^22 for A or 2^38
  *         for D, m or n > 2^24),
  *         INVALID_ARG (NULL pointers, scale format; A and W aligned to 16 bytes with rows of A a multiple of 16 bytes
@@ -593,8 +594,39 @@ mmaemu_status mmaemu_quantize_fp4(const void *x, void *codes, void *scales, void
 mmaemu_status mmaemu_matmul_fp4(const void *A, const void *SA, const void *W, const void *SW, void *D, uint32_t m, uint32_t n,
                                 uint32_t k, uint64_t a_stride, uint64_t d_stride, mmaemu_dtype a_type, mmaemu_dtype d_type,
                                 uint32_t scale_format, float alpha, void *hip_stream);
-/* Name of the kernel that mmaemu_matmul_fp4 takes for these sizes and types ("stream", or "blocks of 256 x 256" and smaller): decided on
- * the host, no GPU needed; for tests and reports. */
+/*
+ * The same three calls with their arguments in a structure (struct_size: its size, reserved: 0).  Bindings that convert arguments one
+ * by one pay for each: from Python the sixteen of a norm took 0.8 us, of 4.5 us for the whole call; as one packed structure 0.3.
+ */
+typedef struct {
+    uint32_t struct_size, cols, type, weight_type, code_type, scale_rule;
+    const void *x, *residual, *weight;
+    void *residual_out, *codes, *scales;
+    uint64_t rows, x_stride, residual_stride;
+    double eps;
+    void *hip_stream;
+} mmaemu_rmsnorm_quantize_args;
+typedef struct {
+    uint32_t struct_size, cols, type, scale_format, scale_rule, reserved;
+    const void *x;
+    void *codes, *scales, *values;
+    uint64_t rows, x_stride;
+    double tensor_scale;
+    void *hip_stream;
+} mmaemu_quantize_fp4_args;
+typedef struct {
+    uint32_t struct_size, m, n, k, a_type, d_type, scale_format, reserved;
+    const void *A, *SA, *W, *SW;
+    void *D;
+    uint64_t a_stride, d_stride;
+    double alpha;
+    void *hip_stream;
+} mmaemu_matmul_fp4_args;
+mmaemu_status mmaemu_rmsnorm_quantize_packed(const mmaemu_rmsnorm_quantize_args *args);
+mmaemu_status mmaemu_quantize_fp4_packed(const mmaemu_quantize_fp4_args *args);
+mmaemu_status mmaemu_matmul_fp4_packed(const mmaemu_matmul_fp4_args *args);
+/* Name of the kernel that mmaemu_matmul_fp4 takes for these sizes and types ("stream", or "blocks of 256 x 256" and smaller; of
+ * two launches the first, larger part's): decided on the host, no GPU needed; for tests and reports. */
 mmaemu_status mmaemu_matmul_fp4_kernel(uint32_t m, uint32_t n, uint32_t k, mmaemu_dtype a_type, uint32_t scale_format, const char **name);
 
 /*

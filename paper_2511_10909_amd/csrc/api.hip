@@ -952,13 +952,47 @@ mmaemu_status mmaemu_matmul_fp4(const void *A, const void *SA, const void *W, co
     return launch_matmul_fp4(A, SA, W, SW, D, m, n, k, a_stride, d_stride, a_type, d_type, scale_format, alpha, (hipStream_t)hip_stream);
 }
 
+// args: an argument structure, whose first field is struct_size
+static bool is_args(const void *args, size_t size, const char *what)
+{
+    if (args && *(const uint32_t *)args == size) return true;
+    set_error("%s: NULL arguments, or a struct_size that is not theirs", what);
+    return false;
+}
+static bool is_zero(uint32_t reserved, const char *what)
+{
+    if (reserved) set_error("%s: reserved must be 0", what);
+    return !reserved;
+}
+
+mmaemu_status mmaemu_rmsnorm_quantize_packed(const mmaemu_rmsnorm_quantize_args *a)
+{
+    if (!is_args(a, sizeof(*a), "rmsnorm_quantize")) return MMAEMU_ERR_INVALID_ARG;
+    return mmaemu_rmsnorm_quantize(a->x, a->residual, a->weight, a->residual_out, a->codes, a->scales, a->rows, a->cols, a->x_stride, a->residual_stride,
+                                   (mmaemu_dtype)a->type, (mmaemu_dtype)a->weight_type, (mmaemu_dtype)a->code_type, a->scale_rule, a->eps, a->hip_stream);
+}
+
+mmaemu_status mmaemu_quantize_fp4_packed(const mmaemu_quantize_fp4_args *a)
+{
+    if (!is_args(a, sizeof(*a), "quantize_fp4") || !is_zero(a->reserved, "quantize_fp4")) return MMAEMU_ERR_INVALID_ARG;
+    return mmaemu_quantize_fp4(a->x, a->codes, a->scales, a->values, a->rows, a->cols, a->x_stride, (mmaemu_dtype)a->type, a->scale_format, a->scale_rule,
+                               (float)a->tensor_scale, a->hip_stream);
+}
+
+mmaemu_status mmaemu_matmul_fp4_packed(const mmaemu_matmul_fp4_args *a)
+{
+    if (!is_args(a, sizeof(*a), "matmul_fp4") || !is_zero(a->reserved, "matmul_fp4")) return MMAEMU_ERR_INVALID_ARG;
+    return mmaemu_matmul_fp4(a->A, a->SA, a->W, a->SW, a->D, a->m, a->n, a->k, a->a_stride, a->d_stride, (mmaemu_dtype)a->a_type, (mmaemu_dtype)a->d_type,
+                             a->scale_format, (float)a->alpha, a->hip_stream);
+}
+
 mmaemu_status mmaemu_matmul_fp4_kernel(uint32_t m, uint32_t n, uint32_t k, mmaemu_dtype a_type, uint32_t scale_format, const char **name)
 {
     if (!name) { set_error("matmul_fp4_kernel: NULL pointer"); return MMAEMU_ERR_INVALID_ARG; }
     uint64_t a_stride = 0, d_stride = 0;
     const mmaemu_status st = check_matmul_fp4(m, n, k, a_stride, d_stride, a_type, MMAEMU_FP32, scale_format, 1.0f);
     if (st != MMAEMU_OK) return st;
-    *name = matmul_fp4_kernel_name(m, n, a_type, scale_format);
+    *name = matmul_fp4_kernel_name(m, n, k, a_type, scale_format);
     return MMAEMU_OK;
 }
 

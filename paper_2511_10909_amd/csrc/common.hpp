@@ -175,7 +175,7 @@ mmaemu_status launch_quantize_fp4(const void *x, void *codes, void *scales, void
                                   uint32_t type, uint32_t scale_format, uint32_t scale_rule, float tensor_scale, hipStream_t s);
 mmaemu_status launch_matmul_fp4(const void *A, const void *SA, const void *W, const void *SW, void *D, uint32_t m, uint32_t n, uint32_t k,
                                 uint64_t a_stride, uint64_t d_stride, uint32_t a_type, uint32_t d_type, uint32_t scale_format, float alpha, hipStream_t s);
-const char *matmul_fp4_kernel_name(uint32_t m, uint32_t n, uint32_t a_type, uint32_t scale_format);
+const char *matmul_fp4_kernel_name(uint32_t m, uint32_t n, uint32_t k, uint32_t a_type, uint32_t scale_format);
 
 // issue-rate probes (issue_rate.hip)
 uint32_t issue_probe_count();

@@ -146,7 +146,7 @@ struct ProductArgs {
 
 // the kernel for many rows of A (matmul_fp4_tiled.hip)
 mmaemu_status launch_tiled(const ProductArgs &p, uint32_t a_type, uint32_t scale_format, hipStream_t s);
-const char *tiled_name(uint32_t m, uint32_t n, uint32_t a_type, uint32_t scale_format);
+const char *tiled_name(uint32_t m, uint32_t n, uint32_t k, uint32_t a_type, uint32_t scale_format);
 
 // four consecutive outputs of one token, columns j .. j + 3, in type DT
 template <int DT> __device__ __forceinline__ void store_outputs(const ProductArgs &p, uint32_t i, uint32_t j, f32x4 v)

@@ -7,17 +7,18 @@ namespace mmaemu {
 // Few tokens: the weights are read once, by the wavefront that multiplies them; nothing is shared but the sum.  A workgroup's
 // wavefronts take the same 16 tokens x 16 NT weight rows and each a contiguous part of the products; their sums meet in LDS.
 //
-// Each wavefront keeps a ring of R slots of DW windows in LDS that only it uses: copies by the memory system fill the slots
+// Each wavefront keeps a ring of two slots of DW windows in LDS that only it uses: copies by the memory system fill the slots
 // ahead, and no barrier is needed.  Loads straight into registers are slower: the instructions want sixteen rows in
 // consecutive lanes, and the first-level cache looks up a line for each lane then, 64 for a load; the copies run along the rows.
-template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> struct Stream {
+template <int AT, int SF, int MR, int NT, int DW, int WAVES> struct Stream {
     static constexpr bool BYTES = AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2;
+    static constexpr int R = 2;                                        // slots (three and four are no faster)
     static constexpr int XB = BYTES ? 128 : 256;                       // bytes of a token per window
     static constexpr int WROW = 64 * DW;                               // bytes of a weight row per slot
     static constexpr int SB = SF == MMAEMU_SCALE_FORMAT_E8M0 ? 4 : 8;  // scale bytes of a weight row per window
     static constexpr int W_BYTES = 16 * NT * WROW, X_BYTES = DW * MR * XB, SLOT = W_BYTES + X_BYTES;
     static constexpr int WC = W_BYTES / 1024, XC = (X_BYTES + 1023) / 1024, COPIES = WC + XC;
-    static constexpr int RUN = 16;                                     // windows whose scales are staged together
+    static constexpr int RUN = 64 / SB;                                // windows whose scales are staged together: 64 bytes of a weight row
     static constexpr int SW_ROW = RUN * SB, SX_ROW = RUN * 4;          // bytes of a row's scales in a run,
     static constexpr int SW_PITCH = SW_ROW + 16, SX_PITCH = SX_ROW + 16;               // and what rows are apart: no two in a bank
     static constexpr int SW_BYTES = 16 * NT * SW_PITCH, SX_BYTES = BYTES ? MR * SX_PITCH : 0;
@@ -60,13 +61,13 @@ template <int AT, int SF> __device__ __forceinline__ f32x4 window_products(u32x4
     return acc;
 }
 
-template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ void __launch_bounds__(64 * WAVES) stream_kernel(const ProductArgs p)
+template <int AT, int SF, int MR, int NT, int DW, int WAVES> __global__ void __launch_bounds__(64 * WAVES) stream_kernel(const ProductArgs p)
 {
-    typedef Stream<AT, SF, MR, NT, DW, R, WAVES> T;
+    typedef Stream<AT, SF, MR, NT, DW, WAVES> T;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15u;
     const uint32_t n0 = blockIdx.x * (16 * NT);
-    uint8_t *const ring = lds + wave * T::WAVE_LDS, *const sw_lds = ring + R * T::SLOT, *const sx_lds = sw_lds + T::SW_BYTES;
+    uint8_t *const ring = lds + wave * T::WAVE_LDS, *const sw_lds = ring + T::R * T::SLOT, *const sx_lds = sw_lds + T::SW_BYTES;
     // this wavefront's slots of the row
     const uint32_t slots = (p.k + 128 * DW - 1) / (128 * DW), per = slots / WAVES, more = slots % WAVES;
     const uint32_t first = wave * per + (wave < more ? wave : more), count = per + (wave < more ? 1 : 0);
@@ -95,10 +96,10 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
         src_k[T::WC + i] = 128 * win + (T::BYTES ? 16 : 8) * c;
     }
     auto issue = [&](uint32_t d) MMAEMU_INLINE {                 // the copies of this wavefront's slot d
-        const uint32_t slot = lds_address(ring) + (d % R) * T::SLOT;
+        const uint32_t slot = lds_address(ring) + (d % T::R) * T::SLOT;
         if ((first + d + 1) * (128 * DW) > p.k) {
             // the slot that ends inside: zeros first, then what is there
-            for (uint32_t c = lane; c < (uint32_t)T::SLOT / 16; c += 64) *reinterpret_cast<u32x4 *>(ring + (d % R) * T::SLOT + 16 * c) = u32x4{0, 0, 0, 0};
+            for (uint32_t c = lane; c < (uint32_t)T::SLOT / 16; c += 64) *reinterpret_cast<u32x4 *>(ring + (d % T::R) * T::SLOT + 16 * c) = u32x4{0, 0, 0, 0};
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
             for (int i = 0; i < T::COPIES; ++i)
@@ -111,7 +112,7 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
         for (int i = 0; i < T::XC; ++i)
             if (src_in[T::WC + i]) copy_to_lds(src[T::WC + i] + (uint64_t)d * (DW * T::XB), slot + T::W_BYTES + 1024 * i);
     };
-    // scales of sixteen windows from this wavefront's slot d on: sixteen bytes per lane, byte by byte at a row's end
+    // scales of a run of windows from this wavefront's slot d on: sixteen bytes per lane, byte by byte at a row's end
     auto stage_scales = [&](uint32_t d) MMAEMU_INLINE {
         constexpr uint32_t W_PIECES = 16 * NT * T::SW_ROW / 16, PIECES = W_PIECES + (T::BYTES ? MR * T::SX_ROW / 16 : 0);
         const uint32_t w0 = (first + d) * DW;      // first window
@@ -141,16 +142,14 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
     f32x4 acc[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[j] = f32x4{0, 0, 0, 0};
-    for (uint32_t d = 0; d < R && d < count; ++d) issue(d);
+    for (uint32_t d = 0; d < T::R && d < count; ++d) issue(d);
     for (uint32_t d = 0; d < count; ++d) {
         if (d % (T::RUN / DW) == 0) stage_scales(d);
-        // slots that may still be under way (one that ends inside counts as none: it may have fewer copies)
-        const uint32_t left = count - d - 1, later = left < R - 1 ? left : R - 1, away = later && later == left && ends_inside ? later - 1 : later;
-        if (away >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * T::COPIES) : "memory");
-        else if (away == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * T::COPIES) : "memory");
-        else if (away == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::COPIES) : "memory");
+        // the next slot may still be under way (one that ends inside counts as none: it may have fewer copies)
+        const uint32_t left = count - d - 1;
+        if (left > 1 || (left == 1 && !ends_inside)) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::COPIES) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        const uint8_t *slot = ring + (d % R) * T::SLOT, *xs = slot + T::W_BYTES;
+        const uint8_t *slot = ring + (d % T::R) * T::SLOT, *xs = slot + T::W_BYTES;
         const uint32_t rx = r % MR;
 #pragma unroll
         for (int h = 0; h < DW; ++h) {
@@ -178,7 +177,7 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // everything of the slot has been read
-        if (d + R < count) issue(d + R);
+        if (d + T::R < count) issue(d + T::R);
     }
     __syncthreads();
     f32x4 *part = reinterpret_cast<f32x4 *>(lds);
@@ -193,11 +192,11 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> __global__ v
     }
 }
 
-template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> static mmaemu_status launch_stream(const ProductArgs &p, hipStream_t s)
+template <int AT, int SF, int MR, int NT, int DW, int WAVES> static mmaemu_status launch_stream(const ProductArgs &p, hipStream_t s)
 {
-    typedef Stream<AT, SF, MR, NT, DW, R, WAVES> T;
-    static_assert(T::LDS <= 160 * 1024 && R <= 4, "ring");
-    hipLaunchKernelGGL((stream_kernel<AT, SF, MR, NT, DW, R, WAVES>), dim3((p.n + 16 * NT - 1) / (16 * NT)), dim3(64 * WAVES), T::LDS, s, p);
+    typedef Stream<AT, SF, MR, NT, DW, WAVES> T;
+    static_assert(T::LDS <= 160 * 1024, "ring");
+    hipLaunchKernelGGL((stream_kernel<AT, SF, MR, NT, DW, WAVES>), dim3((p.n + 16 * NT - 1) / (16 * NT)), dim3(64 * WAVES), T::LDS, s, p);
     MMAEMU_HIP(hipGetLastError());
     return MMAEMU_OK;
 }
@@ -206,21 +205,49 @@ template <int AT, int SF, int MR, int NT, int DW, int R, int WAVES> static mmaem
 // against 8.9 for E4M3 ones; at 32 tokens the stream reads the weights twice).
 constexpr uint32_t STREAM_TOKENS = 16;
 
-// Rows of a slot's activations: those that the tokens fill, 4, 8 (16-bit ones) or 16; fewer cost less of the copies' rate (one BF16 token on
-// 28672 x 8192: 24 us with 2 rows, 37 with 16).  Weight rows: 16 a workgroup until they fill the chip, then more, which share the activations (16 BF16 tokens,
-// n = 4096 / 8192 / 28672, k = 4096 / 8192 / 8192: 5.5, 12.4 and 45 us with 16; 7.3, 10.5 and 39 with 32; 9.9, 13.7 and 33 with 64).  Eight
-// wavefronts instead of four where few workgroups share long rows (one BF16 token, 1024 x 16384: 8.4 -> 6.4 us; 28672 x 8192: 23.8 -> 26.3).
+// Rows of a slot's activations (MR): those that the tokens fill, 4, 8 or 16; fewer cost less of the copies' rate (one BF16 token on
+// 28672 x 8192: 24 us with 4 rows, 37 with 16; 7 E4M3 tokens, 7552 x 3904: 8.5 with 16 rows, 7.4 with 8).
+// Wavefronts: eight instead of four up to 4096 weight rows, where few workgroups share long rows (one BF16 token, 1024 x 16384: 7.0 -> 5.9 us).
+// Windows of a slot (DW): two; four where rows are no whole lines of 128 bytes, as long as all workgroups are resident with them (one E4M3
+// token, 3633 x 4288: 5.8 -> 4.8, 7552 x 3904: 7.1 -> 6.6; but 13824 x 3776: 8.5 -> 10.6).
+// Weight rows of a workgroup (16 NT): 16 until the activations, which every workgroup reads, cost more than idle units, and one window a
+// slot where that is what lets all workgroups be resident.  16-bit activations, us (E8M0 and UE4M3 scales):
+//   7 tokens, 8192 x 8192: 16 rows x 2 windows 7.8 and 8.7, 32 x 2 8.1 and 10.0;  13824 x 3776: 16 x 2 12.1 and 13.1, 16 x 1 10.3 and 10.3,
+//     32 x 2 10.3 and 11.4;  20000 x 5120: 16 x 1 14.0 and 13.7, 32 x 2 18.7 and 16.2;  12864 x 8192: 16 x 1 13.2 and 15.1, 32 x 2 11.5 and 13.5
+//   14 tokens, 7552 x 3904: 16 x 1 8.6 and 8.1, 32 x 1 9.3 and 9.1;  8192 x 8192: 32 x 2 9.1 and 11.0, 32 x 1 9.8 and 10.7, 32 x 1 of eight
+//     wavefronts 10.3 and 10.2;  13824 x 3776: 32 x 1 12.1 and 11.7, 64 x 1 14.0 and 14.4;  28672 x 8192: 64 x 1 34 and 38, 32 x 1 37 and 39;
+//     20000 x 5120 (a few more workgroups than 64 rows each leave resident): 64 x 1 28 and 24, 16 x 1 20 and 17
+// 8-bit ones: 14 tokens, 7552 x 3904: 16 x 2 7.9, 32 x 2 8.6;  13824 x 3776: 12.9 and 10.1;  20000 x 5120: 32 x 2 18.4, 32 x 1 14.2;  28672 x 8192: 27 and 31
 template <int AT, int SF> static mmaemu_status launch_stream_typed(const ProductArgs &p, hipStream_t s)
 {
-    const bool few = p.n < 4096 && p.k >= 4096;
-    if (p.m <= 4) return few ? launch_stream<AT, SF, 4, 1, 2, 2, 8>(p, s) : launch_stream<AT, SF, 4, 1, 2, 2, 4>(p, s);
-    if constexpr (AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2) {
-        if (p.n > 4096) return launch_stream<AT, SF, 16, 2, 2, 2, 4>(p, s);
-        return few ? launch_stream<AT, SF, 16, 1, 2, 2, 8>(p, s) : launch_stream<AT, SF, 16, 1, 2, 2, 4>(p, s);
+    constexpr bool BYTES = AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2, E8M0 = SF == MMAEMU_SCALE_FORMAT_E8M0;
+    const bool few = p.n <= 4096, resident = p.n <= 8192, ragged = p.k % 256 != 0;
+    if (p.m <= 4) {
+        if (few) return ragged ? launch_stream<AT, SF, 4, 1, 4, 8>(p, s) : launch_stream<AT, SF, 4, 1, 2, 8>(p, s);
+        return resident && ragged ? launch_stream<AT, SF, 4, 1, 4, 4>(p, s) : launch_stream<AT, SF, 4, 1, 2, 4>(p, s);
+    }
+    if constexpr (BYTES) {
+        if (p.m <= 8) {
+            if (few) return ragged ? launch_stream<AT, SF, 8, 1, 4, 8>(p, s) : launch_stream<AT, SF, 8, 1, 2, 8>(p, s);
+            return resident && ragged ? launch_stream<AT, SF, 8, 1, 4, 4>(p, s) : launch_stream<AT, SF, 8, 1, 2, 4>(p, s);
+        }
+        if (few) return launch_stream<AT, SF, 16, 1, 2, 8>(p, s);
+        if (resident) return launch_stream<AT, SF, 16, 1, 2, 4>(p, s);
+        return p.n > 16384 && p.n <= 24576 ? launch_stream<AT, SF, 16, 2, 1, 4>(p, s) : launch_stream<AT, SF, 16, 2, 2, 4>(p, s);
     } else {
-        if (p.m <= 8) return p.n < 16384 ? launch_stream<AT, SF, 8, 1, 2, 2, 4>(p, s) : launch_stream<AT, SF, 8, 2, 2, 2, 4>(p, s);
-        if (p.n <= 4096) return launch_stream<AT, SF, 16, 1, 1, 2, 8>(p, s);
-        return p.n < 16384 || p.k < 2048 ? launch_stream<AT, SF, 16, 2, 1, 2, 4>(p, s) : launch_stream<AT, SF, 16, 4, 1, 2, 4>(p, s);
+        if (p.m <= 8) {
+            if (few) return launch_stream<AT, SF, 8, 1, 2, 8>(p, s);
+            if (resident) return launch_stream<AT, SF, 8, 1, 2, 4>(p, s);
+            return p.n <= 20480 && p.k <= 6144 ? launch_stream<AT, SF, 8, 1, 1, 4>(p, s) : launch_stream<AT, SF, 8, 2, 2, 4>(p, s);
+        }
+        if (few) return launch_stream<AT, SF, 16, 1, 1, 8>(p, s);
+        if (resident && p.k <= 4096) return launch_stream<AT, SF, 16, 1, 1, 4>(p, s);
+        if (resident) {
+            if constexpr (E8M0) return launch_stream<AT, SF, 16, 2, 2, 4>(p, s);
+            else return launch_stream<AT, SF, 16, 2, 1, 8>(p, s);
+        }
+        if (p.n <= 16384) return launch_stream<AT, SF, 16, 2, 1, 4>(p, s);
+        return (p.n - 1) % 16384 < 8192 ? launch_stream<AT, SF, 16, 1, 1, 4>(p, s) : launch_stream<AT, SF, 16, 4, 1, 4>(p, s);
     }
 }
 
@@ -239,9 +266,9 @@ mmaemu_status launch_matmul_fp4(const void *A, const void *SA, const void *W, co
     }
 }
 
-const char *matmul_fp4_kernel_name(uint32_t m, uint32_t n, uint32_t a_type, uint32_t scale_format)
+const char *matmul_fp4_kernel_name(uint32_t m, uint32_t n, uint32_t k, uint32_t a_type, uint32_t scale_format)
 {
-    return m > STREAM_TOKENS ? tiled_name(m, n, a_type, scale_format) : "stream";
+    return m > STREAM_TOKENS ? tiled_name(m, n, k, a_type, scale_format) : "stream";
 }
 
 } // namespace mmaemu

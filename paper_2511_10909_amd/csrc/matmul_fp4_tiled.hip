@@ -14,8 +14,8 @@ template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S> struct 
     static constexpr int WB = PART / 2;                                // bytes of a weight row in a part
     static constexpr int PER_SCALE = SF == MMAEMU_SCALE_FORMAT_E8M0 ? 32 : 16;
     static constexpr int SB = PART / PER_SCALE;                        // scale bytes of a row in a part
+    static constexpr bool IN_REGISTERS = SB * WK <= 4;                 // scales staged through registers (else by copies, as aligned words)
     static constexpr int GB = SB * WK < 16 ? 16 : SB * WK, GROUP = GB / (SB * WK);     // scale bytes of a row staged together, and their steps
-    static constexpr bool IN_REGISTERS = GROUP >= 4;                   // staged through registers (else by copies, as aligned words)
     static constexpr int WPR = IN_REGISTERS ? GB / 4 : GB / 4 + 1;     // words of a row's scales in LDS
     static constexpr int BLOCKS_M = BM / TM, BLOCKS = BLOCKS_M * (BN / TN), THREADS = 64 * BLOCKS * WK;
     static constexpr int A_PART = BM * 128, W_PART = BN * WB, A_BYTES = A_PART * WK, W_BYTES = W_PART * WK, STAGE = A_BYTES + W_BYTES;
@@ -27,6 +27,16 @@ template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S> struct 
     // copy the same twice), as each counts its own
     static constexpr int AC = (A_BYTES / 16 + THREADS - 1) / THREADS, WC = (W_BYTES / 16 + THREADS - 1) / THREADS, COPIES = AC + WC;
 };
+
+// waits until at most `steps` (up to MOST) steps of EACH copies, of those issued last, are under way
+template <int MOST, int EACH> __device__ __forceinline__ void wait_copies(uint32_t steps)
+{
+    if constexpr (MOST > 0) {
+        if (steps < MOST) return wait_copies<MOST - 1, EACH>(steps);
+    }
+    static_assert(MOST * EACH < 64, "the counter's range");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(MOST * EACH) : "memory");
+}
 
 template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S, bool PIPE>
 __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)) tiled_kernel(const ProductArgs p, uint32_t tiles_m, uint32_t tiles_n)
@@ -258,7 +268,7 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
         }
     };
 
-    static_assert(S <= 3, "waits for one step or none under way");
+    static_assert(T::IN_REGISTERS || T::GROUP >= S - 2, "a group's scales have come with the step that they are first read in");
     // The step that is read next: its buffer and its place among the scales.
     uint32_t at = 0, in_group = 0, half = 0;
     auto go_on = [&]() MMAEMU_INLINE {
@@ -276,8 +286,7 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
         else {
             if (in_group == 0 && s && s / T::GROUP >= copied_groups) put_scales(half);         // (into the half that was read a group ago)
             // (a step that ends inside counts as none: it may have fewer copies)
-            if (S == 3 && (steady || s + 1 < whole_steps)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S - 2) * T::COPIES) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            wait_copies<S - 2, T::COPIES>(steady || s + (S - 2) < whole_steps ? S - 2 : s < whole_steps ? whole_steps - 1 - s : 0);
         }
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -372,59 +381,137 @@ template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S, bool PI
 }
 
 // Which block: the one whose rounds of workgroups over the 256 compute units take least, by what one round and two rounds took (us
-// for 8192 products, E4M3 and BF16 activations on MXFP4 weights; of some blocks two workgroups fit a unit).  A larger block reads
-// less per product, a smaller one fills the chip with fewer tokens and splits its products among more wavefronts.  Both sides
-// where the choice changes, E4M3 and BF16, us:
+// for 2048 and 8192 products, E4M3 and BF16 activations on MXFP4 weights, 8192 weight rows; of some blocks two workgroups fit a unit).
+// Between and beyond these lengths the time is a straight line, below them that of 2048.  A larger block reads less per product, a smaller
+// one fills the chip with fewer tokens and splits its products among more wavefronts.  Both sides where the choice changes, E4M3 and BF16, us:
 //   2048 tokens, 8192 x 4096: 256 x 256 62 and 115, 128 x 256 70 and 132;  256 tokens, 28672 x 8192: 128 x 256 68 and 127, 256 x 256 103 and 215
-//   512 tokens, 8192 x 8192: 128 x 128 37 and 67, 64 x 128 41 and 76;      256 tokens: 64 x 128 25 and 46, 64 x 64 27 (E4M3), 32 x 64 53 (BF16), 128 x 128 35 and 66
-//   128 tokens: 64 x 64 18 (E4M3), 32 x 64 23 and 28, 64 x 128 23 and 46;  64 tokens: 32 x 64 13 and 19, 64 x 64 17 (E4M3), 32 x 32 17 and 23;  32 tokens: 32 x 32 11 and 13, 32 x 64 13 and 19
-struct BlockChoice { uint32_t bm, bn; float one[2], two[2]; };                // (0: not built for 16-bit activations, where 32 x 64 or 64 x 128 takes less anywhere)
+//   512 tokens, 8192 x 8192: 128 x 128 36 and 63, 64 x 128 45 and 66;      8192 x 2048: 128 x 128 15 and 23, 64 x 128 17 and 21
+//   256 tokens, 8192 x 8192: 64 x 128 23 and 38, 64 x 64 26 and 43, 128 x 128 35 and 61
+//   128 tokens: 64 x 64 16 and 22, 32 x 64 22 and 26;  64 tokens: 32 x 64 12 and 16, 64 x 64 16 (E4M3), 32 x 32 17 and 23;  32 tokens: 32 x 32 10 and 12, 32 x 64 12 and 16
+struct BlockTimes { float one[2], two[2]; };       // [0]: 8-bit activations, [1]: 16-bit ones
+struct BlockChoice { uint32_t bm, bn; BlockTimes at_2048, at_8192; };
 static const BlockChoice BLOCK_CHOICES[] = {
-    {256, 256, {112, 225}, {224, 450}}, {128, 256, {65, 126}, {130, 252}}, {128, 128, {37, 67}, {74, 134}}, {64, 128, {24.6f, 46}, {48, 76}},
-    {64, 64, {17.6f, 0}, {27.4f, 0}}, {32, 64, {13.4f, 19.3f}, {23, 27.8f}}, {32, 32, {11, 13.3f}, {17, 23.4f}},
+    {256, 256, {{34.6f, 66.7f}, {66, 128}}, {{102, 213}, {205, 411}}},
+    {128, 256, {{22.5f, 36.5f}, {40.4f, 69}}, {{62, 117}, {119, 237}}},
+    {128, 128, {{14.9f, 23}, {25.9f, 42.6f}}, {{35.5f, 63}, {69, 123}}},
+    {64, 128, {{9.8f, 13.2f}, {17.2f, 20.9f}}, {{22.9f, 38}, {44.5f, 66}}},
+    {64, 64, {{7.3f, 11.2f}, {9.9f, 17.9f}}, {{15.8f, 22.3f}, {26.2f, 42.5f}}},
+    {32, 64, {{6.1f, 7.5f}, {10.3f, 9.7f}}, {{12.4f, 15.9f}, {22.3f, 25.8f}}},
+    {32, 32, {{5.7f, 6.8f}, {9.3f, 10.6f}}, {{10.3f, 11.8f}, {16.5f, 21.6f}}},
 };
+constexpr uint32_t BLOCK_KINDS = sizeof(BLOCK_CHOICES) / sizeof(BLOCK_CHOICES[0]), UNITS = 256;
 
-static uint32_t choose_block(uint32_t m, uint32_t n, bool bytes, bool fp16_e8m0)
+static uint32_t blocks_along(uint32_t size, uint32_t block) { return (size + block - 1) / block; }
+
+static float block_time(const BlockChoice &b, uint32_t m, uint32_t n, uint32_t k, bool bytes)
 {
-    uint32_t best = 0;
-    float least = 0;
-    for (uint32_t i = fp16_e8m0 ? 1 : 0; i < sizeof(BLOCK_CHOICES) / sizeof(BLOCK_CHOICES[0]); ++i) {      // (FP16 activations' second way leaves too few registers for 256 x 256)
-        const BlockChoice &b = BLOCK_CHOICES[i];
-        if (b.one[bytes ? 0 : 1] == 0) continue;
-        const uint64_t tiles = (uint64_t)((m + b.bm - 1) / b.bm) * ((n + b.bn - 1) / b.bn);
-        const uint64_t rounds = (tiles + 255) / 256;
-        const float t = b.two[bytes ? 0 : 1] * (float)(rounds / 2) + (rounds % 2 ? b.one[bytes ? 0 : 1] : 0.0f);
-        if (least == 0 || t < least) {
+    const uint64_t rounds = ((uint64_t)blocks_along(m, b.bm) * blocks_along(n, b.bn) + UNITS - 1) / UNITS;
+    const int type = bytes ? 0 : 1;
+    const auto of = [&](const BlockTimes &t) { return t.two[type] * (float)(rounds / 2) + (rounds % 2 ? t.one[type] : 0.0f); };
+    const float brief = of(b.at_2048), slope = (of(b.at_8192) - brief) / 6144;
+    return k > 2048 ? brief + slope * (float)(k - 2048) : brief;
+}
+
+// `time`: what it takes; FP16 activations' second way under E8M0 scales leaves too few registers for 256 x 256
+static uint32_t choose_block(uint32_t m, uint32_t n, uint32_t k, bool bytes, bool fp16_e8m0, float *time = nullptr)
+{
+    uint32_t best = fp16_e8m0 ? 1 : 0;
+    float least = block_time(BLOCK_CHOICES[best], m, n, k, bytes);
+    for (uint32_t i = best + 1; i < BLOCK_KINDS; ++i) {
+        const float t = block_time(BLOCK_CHOICES[i], m, n, k, bytes);
+        if (t < least) {
             least = t;
             best = i;
         }
     }
+    if (time) *time = least;
     return best;
 }
 
-const char *tiled_name(uint32_t m, uint32_t n, uint32_t a_type, uint32_t scale_format)
+// Blocks that fill some rounds and leave a few for one more cost that whole round.  Where it takes less, whole rounds go first, as a
+// product with fewer weight rows or tokens, and what is left follows in blocks of its own choice, in a second launch; the parts have to be
+// expected to take a twentieth less, and 3 us (1294 E5M2 tokens, 24384 x 5568: 252 us in one launch, 188 in two; 6639 E4M3 tokens, 2432 x 1888:
+// 59 and 45; but 1648 BF16 tokens, 3010 x 544: 15.6 and 18.4).
+struct Split { uint32_t m, n, block; };            // the first part (all of it: one launch)
+
+static Split choose_split(uint32_t m, uint32_t n, uint32_t k, bool bytes, bool fp16_e8m0)
 {
-    static const char *const names[] = {"blocks of 256 x 256", "blocks of 128 x 256", "blocks of 128 x 128", "blocks of 64 x 128", "blocks of 64 x 64", "blocks of 32 x 64", "blocks of 32 x 32"};
-    return names[choose_block(m, n, is_byte_type(a_type), a_type == MMAEMU_FP16 && scale_format == MMAEMU_SCALE_FORMAT_E8M0)];
+    float whole;
+    Split best = {m, n, choose_block(m, n, k, bytes, fp16_e8m0, &whole)};
+    const float few = 3.0f * (k < 2048 ? 2048.0f / (float)k : 1.0f);  // (block_time is that of 2048 products there)
+    float least = whole - (few > 0.05f * whole ? few : 0.05f * whole);
+    for (uint32_t i = fp16_e8m0 ? 1 : 0; i < BLOCK_KINDS; ++i) {
+        const BlockChoice &b = BLOCK_CHOICES[i];
+        const uint32_t tm = blocks_along(m, b.bm), tn = blocks_along(n, b.bn);
+        const uint64_t rounds = (uint64_t)tm * tn / UNITS;
+        const auto consider = [&](uint64_t m1, uint64_t n1) {
+            if (!rounds || !m1 || !n1 || m1 > m || n1 > n || (m1 == m && n1 == n)) return;
+            float rest;
+            choose_block(m1 < m ? m - (uint32_t)m1 : m, n1 < n ? n - (uint32_t)n1 : n, k, bytes, fp16_e8m0, &rest);
+            const float t = block_time(b, (uint32_t)m1, (uint32_t)n1, k, bytes) + rest;
+            if (t < least) {
+                least = t;
+                best = {(uint32_t)m1, (uint32_t)n1, i};
+            }
+        };
+        consider(m, UNITS * rounds / tm * b.bn);
+        consider(UNITS * rounds / tn * b.bm, n);
+    }
+    return best;
 }
 
-template <int AT, int SF> static mmaemu_status launch_tiled_typed(const ProductArgs &p, hipStream_t s)
+static bool two_ways(uint32_t a_type, uint32_t scale_format) { return a_type == MMAEMU_FP16 && scale_format == MMAEMU_SCALE_FORMAT_E8M0; }
+
+const char *tiled_name(uint32_t m, uint32_t n, uint32_t k, uint32_t a_type, uint32_t scale_format)
+{
+    static const char *const names[] = {"blocks of 256 x 256", "blocks of 128 x 256", "blocks of 128 x 128", "blocks of 64 x 128", "blocks of 64 x 64", "blocks of 32 x 64", "blocks of 32 x 32"};
+    return names[choose_split(m, n, k, is_byte_type(a_type), two_ways(a_type, scale_format)).block];
+}
+
+template <int AT, int SF> static mmaemu_status launch_block(const ProductArgs &p, uint32_t block, hipStream_t s)
 {
     constexpr bool BYTES = AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2, TWO_WAYS = AT == MMAEMU_FP16 && SF == MMAEMU_SCALE_FORMAT_E8M0;
-    switch (choose_block(p.m, p.n, BYTES, TWO_WAYS)) {
-    // (the wavefront's share, the depth of the buffers and the reading ahead: what was fastest for each kind of activations; wavefronts that
-    // take weights to 16 bits have fewer of them and more tokens: 2048 x 8192 x 4096 under UE4M3 scales 191 -> 144 us)
+    switch (block) {
+    // (the wavefront's share, the depth of the buffers and the reading ahead: what was fastest for each kind of activations; deeper buffers
+    // than three gain nothing; wavefronts that take weights to 16 bits have fewer of them and more tokens: 2048 x 8192 x 4096 under UE4M3
+    // scales 191 -> 144 us; 128 BF16 tokens on 8192 x 8192 in 64 x 64: 30 us with 32 x 32 a wavefront, 22 with 64 x 32)
     case 0:
         if constexpr (BYTES) return launch_tile<AT, SF, 256, 256, 64, 128, 1, 3, false>(p, s);
         else if constexpr (!TWO_WAYS) return launch_tile<AT, SF, 256, 256, 128, 64, 1, 3, false>(p, s);
     case 1: return launch_tile<AT, SF, 128, 256, 64, 64, 1, 3, !BYTES && !TWO_WAYS>(p, s);
     case 2: return launch_tile<AT, SF, 128, 128, 64, 64, 2, 3, !BYTES && !TWO_WAYS>(p, s);
-    case 3: return launch_tile<AT, SF, 64, 128, 64, 32, 2, BYTES ? 3 : 2, false>(p, s);
+    case 3: return launch_tile<AT, SF, 64, 128, 64, 32, 2, TWO_WAYS ? 2 : 3, false>(p, s);
     case 4:
         if constexpr (BYTES) return launch_tile<AT, SF, 64, 64, 32, 32, 2, 3, false>(p, s);
+        else return launch_tile<AT, SF, 64, 64, 64, 32, 4, 3, !TWO_WAYS>(p, s);
     case 5: return launch_tile<AT, SF, 32, 64, 32, 32, 4, 3, false>(p, s);
     default: return launch_tile<AT, SF, 32, 32, 32, 32, 8, 3, false>(p, s);
     }
+}
+
+template <int AT, int SF> static mmaemu_status launch_tiled_typed(const ProductArgs &p, hipStream_t s)
+{
+    constexpr bool BYTES = AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2, TWO_WAYS = AT == MMAEMU_FP16 && SF == MMAEMU_SCALE_FORMAT_E8M0;
+    const Split first = choose_split(p.m, p.n, p.k, BYTES, TWO_WAYS);
+    ProductArgs part = p;
+    part.m = first.m;
+    part.n = first.n;
+    const mmaemu_status st = launch_block<AT, SF>(part, first.block, s);
+    if (st != MMAEMU_OK || (first.m == p.m && first.n == p.n)) return st;
+    const uint64_t eb = p.d_type == MMAEMU_FP32 ? 4 : 2;
+    part = p;
+    if (first.m < p.m) {
+        part.m = p.m - first.m;
+        part.A = p.A + first.m * p.a_stride;
+        if (BYTES) part.SA = p.SA + (uint64_t)first.m * (p.k / 32);
+        part.D = (char *)p.D + first.m * p.d_stride * eb;
+    } else {
+        part.n = p.n - first.n;
+        part.W = p.W + (uint64_t)first.n * (p.k / 2);
+        part.SW = p.SW + (uint64_t)first.n * (p.k / (SF == MMAEMU_SCALE_FORMAT_E8M0 ? 32 : 16));
+        part.D = (char *)p.D + first.n * eb;
+    }
+    return launch_block<AT, SF>(part, choose_block(part.m, part.n, p.k, BYTES, TWO_WAYS), s);
 }
 
 mmaemu_status launch_tiled(const ProductArgs &p, uint32_t a_type, uint32_t scale_format, hipStream_t s)

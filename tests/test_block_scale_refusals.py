@@ -1,5 +1,6 @@
 """Arguments that the block-scaled operators refuse, and calls that are no-ops: decided on the host, no GPU needed."""
 import math
+import struct
 
 import pytest
 
@@ -69,3 +70,21 @@ def test_kernel_names_of_products():
         with pytest.raises(mm.MmaemuError) as e:
             mm.matmul_fp4_kernel(*args)
         assert e.value.status == status
+
+
+def test_argument_structures():
+    """The binding's packed structures are the header's, and one of another size is refused."""
+    assert (mm._NORM_ARGS.size, mm._QUANTIZE_ARGS.size, mm._MATMUL_ARGS.size) == (112, 88, 104)
+    for fn, packed in ((mm._norm_call, mm._NORM_ARGS), (mm._quantize_call, mm._QUANTIZE_ARGS), (mm._matmul_call, mm._MATMUL_ARGS)):
+        assert fn(None) == INVALID
+        for size in (0, packed.size - 8, packed.size + 8):
+            assert fn(size.to_bytes(4, "little") + bytes(packed.size - 4)) == INVALID
+
+
+def test_numbers_that_no_argument_holds():
+    for kw in (dict(m=1 << 32), dict(n=-1), dict(a_stride=-64), dict(k=64.0)):
+        a = dict(A=P, SA=None, W=P, SW=P, D=P, m=3, n=5, k=64, a_type=mm.BF16, d_type=mm.BF16)
+        a.update(kw)
+        with pytest.raises(struct.error):
+            mm.matmul_fp4(**a, stream=0)
+    refused(INVALID, mm.matmul_fp4, A=P, SA=None, W=P, SW=P, D=P, m=3, n=5, k=64, a_type=mm.BF16, d_type=mm.BF16, alpha=1e39)

@@ -386,18 +386,18 @@ template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S, bool PI
 // one fills the chip with fewer tokens and splits its products among more wavefronts.  Both sides where the choice changes, E4M3 and BF16, us:
 //   2048 tokens, 8192 x 4096: 256 x 256 62 and 115, 128 x 256 70 and 132;  256 tokens, 28672 x 8192: 128 x 256 68 and 127, 256 x 256 103 and 215
 //   512 tokens, 8192 x 8192: 128 x 128 36 and 63, 64 x 128 45 and 66;      8192 x 2048: 128 x 128 15 and 23, 64 x 128 17 and 21
-//   256 tokens, 8192 x 8192: 64 x 128 23 and 38, 64 x 64 26 and 43, 128 x 128 35 and 61
-//   128 tokens: 64 x 64 16 and 22, 32 x 64 22 and 26;  64 tokens: 32 x 64 12 and 16, 64 x 64 16 (E4M3), 32 x 32 17 and 23;  32 tokens: 32 x 32 10 and 12, 32 x 64 12 and 16
+//   256 tokens, 8192 x 8192: 64 x 128 23 and 36, 64 x 64 26 and 43, 128 x 128 35 and 61
+//   128 tokens: 64 x 64 16 and 22, 32 x 64 21 and 26;  64 tokens: 32 x 64 12 and 16, 64 x 64 16 and 21, 32 x 32 15 and 22;  32 tokens: 32 x 32 9.5 and 12, 32 x 64 12 and 16
 struct BlockTimes { float one[2], two[2]; };       // [0]: 8-bit activations, [1]: 16-bit ones
 struct BlockChoice { uint32_t bm, bn; BlockTimes at_2048, at_8192; };
 static const BlockChoice BLOCK_CHOICES[] = {
     {256, 256, {{34.6f, 66.7f}, {66, 128}}, {{102, 213}, {205, 411}}},
     {128, 256, {{22.5f, 36.5f}, {40.4f, 69}}, {{62, 117}, {119, 237}}},
     {128, 128, {{14.9f, 23}, {25.9f, 42.6f}}, {{35.5f, 63}, {69, 123}}},
-    {64, 128, {{9.8f, 13.2f}, {17.2f, 20.9f}}, {{22.9f, 38}, {44.5f, 66}}},
+    {64, 128, {{9.8f, 13.2f}, {17.2f, 20.9f}}, {{22.9f, 35.5f}, {44.5f, 66}}},
     {64, 64, {{7.3f, 11.2f}, {9.9f, 17.9f}}, {{15.8f, 22.3f}, {26.2f, 42.5f}}},
-    {32, 64, {{6.1f, 7.5f}, {10.3f, 9.7f}}, {{12.4f, 15.9f}, {22.3f, 25.8f}}},
-    {32, 32, {{5.7f, 6.8f}, {9.3f, 10.6f}}, {{10.3f, 11.8f}, {16.5f, 21.6f}}},
+    {32, 64, {{5.8f, 7.5f}, {9.8f, 9.7f}}, {{11.8f, 15.9f}, {21.4f, 25.8f}}},
+    {32, 32, {{5.1f, 6.8f}, {8, 10.6f}}, {{9.5f, 11.8f}, {15, 21.6f}}},
 };
 constexpr uint32_t BLOCK_KINDS = sizeof(BLOCK_CHOICES) / sizeof(BLOCK_CHOICES[0]), UNITS = 256;
 
@@ -474,18 +474,23 @@ template <int AT, int SF> static mmaemu_status launch_block(const ProductArgs &p
     switch (block) {
     // (the wavefront's share, the depth of the buffers and the reading ahead: what was fastest for each kind of activations; deeper buffers
     // than three gain nothing; wavefronts that take weights to 16 bits have fewer of them and more tokens: 2048 x 8192 x 4096 under UE4M3
-    // scales 191 -> 144 us; 128 BF16 tokens on 8192 x 8192 in 64 x 64: 30 us with 32 x 32 a wavefront, 22 with 64 x 32)
+    // scales 191 -> 144 us; 8-bit ones have no such work, and sixteen wavefronts in the smallest blocks: 64 E4M3 tokens on 8192 x 8192 12.7 ->
+    // 11.8, 16-bit ones 16.2 -> 18.3; 128 BF16 tokens on 8192 x 8192 in 64 x 64: 30 us with 32 x 32 a wavefront, 22 with 64 x 32)
     case 0:
         if constexpr (BYTES) return launch_tile<AT, SF, 256, 256, 64, 128, 1, 3, false>(p, s);
         else if constexpr (!TWO_WAYS) return launch_tile<AT, SF, 256, 256, 128, 64, 1, 3, false>(p, s);
     case 1: return launch_tile<AT, SF, 128, 256, 64, 64, 1, 3, !BYTES && !TWO_WAYS>(p, s);
     case 2: return launch_tile<AT, SF, 128, 128, 64, 64, 2, 3, !BYTES && !TWO_WAYS>(p, s);
-    case 3: return launch_tile<AT, SF, 64, 128, 64, 32, 2, TWO_WAYS ? 2 : 3, false>(p, s);
+    case 3:
+        // (one round: sixteen wavefronts a unit, 256 BF16 tokens on 8192 x 8192 39 -> 35 us; two: two workgroups of eight, 512 tokens 71 -> 66)
+        if constexpr (!BYTES && !TWO_WAYS)
+            if ((uint64_t)blocks_along(p.m, 64) * blocks_along(p.n, 128) <= UNITS) return launch_tile<AT, SF, 64, 128, 64, 32, 4, 3, false>(p, s);
+        return launch_tile<AT, SF, 64, 128, 64, 32, 2, TWO_WAYS ? 2 : 3, false>(p, s);
     case 4:
         if constexpr (BYTES) return launch_tile<AT, SF, 64, 64, 32, 32, 2, 3, false>(p, s);
         else return launch_tile<AT, SF, 64, 64, 64, 32, 4, 3, !TWO_WAYS>(p, s);
-    case 5: return launch_tile<AT, SF, 32, 64, 32, 32, 4, 3, false>(p, s);
-    default: return launch_tile<AT, SF, 32, 32, 32, 32, 8, 3, false>(p, s);
+    case 5: return launch_tile<AT, SF, 32, 64, 32, BYTES ? 16 : 32, 4, 3, false>(p, s);
+    default: return launch_tile<AT, SF, 32, 32, 32, BYTES ? 16 : 32, 8, 3, false>(p, s);
     }
 }
 

@@ -38,7 +38,13 @@ template <int MOST, int EACH> __device__ __forceinline__ void wait_copies(uint32
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(MOST * EACH) : "memory");
 }
 
-template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S, bool PIPE>
+// How a wavefront's reads from LDS and its matrix instructions follow one another: a step's reads before its products; the next step's reads
+// before them; or the workgroup's eight wavefronts in two halves, one of each on every SIMD, that take turns: while one reads, the other
+// multiplies (8192 x 8192 outputs, 8192 products, in order and by turns: E4M3 437 -> 403 us, BF16 872 -> 789 in 256 x 256; 252 -> 244
+// and, from reading ahead, 480 -> 475 for half the rows in 128 x 256).
+enum class Order { PLAIN, AHEAD, TURNS };
+
+template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S, Order ORDER>
 __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)) tiled_kernel(const ProductArgs p, uint32_t tiles_m, uint32_t tiles_n)
 {
     typedef Tile<AT, SF, BM, BN, TM, TN, WK, S> T;
@@ -296,6 +302,7 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
         }
     };
     // steps before which all that is waited for or issued is whole
+    constexpr bool PIPE = ORDER == Order::AHEAD;
     constexpr uint32_t AHEAD = PIPE ? S : S - 1;   // steps issued ahead of the one that is multiplied
     uint32_t steady_steps = whole_steps > AHEAD ? whole_steps - AHEAD : 0;
     if (!T::IN_REGISTERS) {
@@ -332,6 +339,43 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
             step(one, two, std::false_type());
             if (s < steps) step(two, one, std::false_type());
         }
+    } else if constexpr (ORDER == Order::TURNS) {
+        static_assert(T::THREADS == 512 && S == 3 && T::IN_REGISTERS && T::GROUP > 1, "two halves of four wavefronts");
+        // Between barriers 2 s and 2 s + 1 the first half reads step s and issues the copies of step s + 2, while the second multiplies
+        // step s - 1; then they change places.  The copies go into the buffer of step s - 1, which the second half has read before barrier
+        // 2 s.  What step s + 1 needs of a wavefront (its copies, its scales) is there before barrier 2 s + 2.
+        const bool second = wave >= 4;
+        auto turn = [&]() MMAEMU_INLINE {
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto ready = [&](auto steady) MMAEMU_INLINE {            // what this wavefront brings for step s + 1
+            wait_copies<1, T::COPIES>(steady || s + 2 < whole_steps ? 1 : 0);
+            if (in_group == 0 && (steady || s + 1 + T::GROUP < steps)) load_scales();
+        };
+        auto step = [&](auto steady) MMAEMU_INLINE {
+            if (in_group + 1 == T::GROUP && (steady || s + 1 < steps)) put_scales(half ^ T::SCALES);
+            if (steady || s + 2 < steps) issue(steady || s + 2 < whole_steps);
+            Part q;
+            read_part(q, at, half, in_group);
+            go_on();
+            if (second) ready(steady);
+            turn();
+            multiply(q);
+            if (!second) ready(steady);
+            turn();
+            ++s;
+        };
+        wait_copies<1, T::COPIES>(whole_steps > 1 ? 1 : 0);
+        if (T::GROUP < steps) load_scales();
+        turn();
+        if (second) turn();
+        while (s < steady_steps) step(std::true_type());
+        while (s < steps) step(std::false_type());
+        if (!second) turn();
     } else {
         auto step = [&](auto steady) MMAEMU_INLINE {
             arrive(s, steady);
@@ -370,12 +414,12 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
     });
 }
 
-template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S, bool PIPE> static mmaemu_status launch_tile(const ProductArgs &p, hipStream_t s)
+template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S, Order ORDER> static mmaemu_status launch_tile(const ProductArgs &p, hipStream_t s)
 {
     typedef Tile<AT, SF, BM, BN, TM, TN, WK, S> T;
     const uint32_t tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
     static_assert(T::LDS <= 160 * 1024 && (T::A_BYTES / 16) % 64 == 0 && (T::W_BYTES / 16) % 64 == 0, "tile");
-    hipLaunchKernelGGL((tiled_kernel<AT, SF, BM, BN, TM, TN, WK, S, PIPE>), dim3(tm * tn), dim3(T::THREADS), T::LDS, s, p, tm, tn);
+    hipLaunchKernelGGL((tiled_kernel<AT, SF, BM, BN, TM, TN, WK, S, ORDER>), dim3(tm * tn), dim3(T::THREADS), T::LDS, s, p, tm, tn);
     MMAEMU_HIP(hipGetLastError());
     return MMAEMU_OK;
 }
@@ -384,15 +428,15 @@ template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S, bool PI
 // for 2048 and 8192 products, E4M3 and BF16 activations on MXFP4 weights, 8192 weight rows; of some blocks two workgroups fit a unit).
 // Between and beyond these lengths the time is a straight line, below them that of 2048.  A larger block reads less per product, a smaller
 // one fills the chip with fewer tokens and splits its products among more wavefronts.  Both sides where the choice changes, E4M3 and BF16, us:
-//   2048 tokens, 8192 x 4096: 256 x 256 62 and 115, 128 x 256 70 and 132;  256 tokens, 28672 x 8192: 128 x 256 68 and 127, 256 x 256 103 and 215
+//   2048 tokens, 8192 x 4096: 256 x 256 54 and 102, 128 x 256 66 and 122;  256 tokens, 28672 x 8192: 128 x 256 66 and 123, 256 x 256 100 and 198
 //   512 tokens, 8192 x 8192: 128 x 128 36 and 63, 64 x 128 45 and 66;      8192 x 2048: 128 x 128 15 and 23, 64 x 128 17 and 21
 //   256 tokens, 8192 x 8192: 64 x 128 23 and 36, 64 x 64 26 and 43, 128 x 128 35 and 61
 //   128 tokens: 64 x 64 16 and 22, 32 x 64 21 and 26;  64 tokens: 32 x 64 12 and 16, 64 x 64 16 and 21, 32 x 32 15 and 22;  32 tokens: 32 x 32 9.5 and 12, 32 x 64 12 and 16
 struct BlockTimes { float one[2], two[2]; };       // [0]: 8-bit activations, [1]: 16-bit ones
 struct BlockChoice { uint32_t bm, bn; BlockTimes at_2048, at_8192; };
 static const BlockChoice BLOCK_CHOICES[] = {
-    {256, 256, {{34.6f, 66.7f}, {66, 128}}, {{102, 213}, {205, 411}}},
-    {128, 256, {{22.5f, 36.5f}, {40.4f, 69}}, {{62, 117}, {119, 237}}},
+    {256, 256, {{33.5f, 58}, {64, 111}}, {{94, 190}, {193, 376}}},
+    {128, 256, {{22.5f, 35.5f}, {40.4f, 67}}, {{60, 113}, {116, 232}}},
     {128, 128, {{14.9f, 23}, {25.9f, 42.6f}}, {{35.5f, 63}, {69, 123}}},
     {64, 128, {{9.8f, 13.2f}, {17.2f, 20.9f}}, {{22.9f, 35.5f}, {44.5f, 66}}},
     {64, 64, {{7.3f, 11.2f}, {9.9f, 17.9f}}, {{15.8f, 22.3f}, {26.2f, 42.5f}}},
@@ -477,20 +521,20 @@ template <int AT, int SF> static mmaemu_status launch_block(const ProductArgs &p
     // scales 191 -> 144 us; 8-bit ones have no such work, and sixteen wavefronts in the smallest blocks: 64 E4M3 tokens on 8192 x 8192 12.7 ->
     // 11.8, 16-bit ones 16.2 -> 18.3; 128 BF16 tokens on 8192 x 8192 in 64 x 64: 30 us with 32 x 32 a wavefront, 22 with 64 x 32)
     case 0:
-        if constexpr (BYTES) return launch_tile<AT, SF, 256, 256, 64, 128, 1, 3, false>(p, s);
-        else if constexpr (!TWO_WAYS) return launch_tile<AT, SF, 256, 256, 128, 64, 1, 3, false>(p, s);
-    case 1: return launch_tile<AT, SF, 128, 256, 64, 64, 1, 3, !BYTES && !TWO_WAYS>(p, s);
-    case 2: return launch_tile<AT, SF, 128, 128, 64, 64, 2, 3, !BYTES && !TWO_WAYS>(p, s);
+        if constexpr (BYTES) return launch_tile<AT, SF, 256, 256, 64, 128, 1, 3, Order::TURNS>(p, s);
+        else if constexpr (!TWO_WAYS) return launch_tile<AT, SF, 256, 256, 128, 64, 1, 3, Order::TURNS>(p, s);
+    case 1: return launch_tile<AT, SF, 128, 256, 64, 64, 1, 3, TWO_WAYS ? Order::PLAIN : Order::TURNS>(p, s);
+    case 2: return launch_tile<AT, SF, 128, 128, 64, 64, 2, 3, !BYTES && !TWO_WAYS ? Order::AHEAD : Order::PLAIN>(p, s);
     case 3:
         // (one round: sixteen wavefronts a unit, 256 BF16 tokens on 8192 x 8192 39 -> 35 us; two: two workgroups of eight, 512 tokens 71 -> 66)
         if constexpr (!BYTES && !TWO_WAYS)
-            if ((uint64_t)blocks_along(p.m, 64) * blocks_along(p.n, 128) <= UNITS) return launch_tile<AT, SF, 64, 128, 64, 32, 4, 3, false>(p, s);
-        return launch_tile<AT, SF, 64, 128, 64, 32, 2, TWO_WAYS ? 2 : 3, false>(p, s);
+            if ((uint64_t)blocks_along(p.m, 64) * blocks_along(p.n, 128) <= UNITS) return launch_tile<AT, SF, 64, 128, 64, 32, 4, 3, Order::PLAIN>(p, s);
+        return launch_tile<AT, SF, 64, 128, 64, 32, 2, TWO_WAYS ? 2 : 3, Order::PLAIN>(p, s);
     case 4:
-        if constexpr (BYTES) return launch_tile<AT, SF, 64, 64, 32, 32, 2, 3, false>(p, s);
-        else return launch_tile<AT, SF, 64, 64, 64, 32, 4, 3, !TWO_WAYS>(p, s);
-    case 5: return launch_tile<AT, SF, 32, 64, 32, BYTES ? 16 : 32, 4, 3, false>(p, s);
-    default: return launch_tile<AT, SF, 32, 32, 32, BYTES ? 16 : 32, 8, 3, false>(p, s);
+        if constexpr (BYTES) return launch_tile<AT, SF, 64, 64, 32, 32, 2, 3, Order::PLAIN>(p, s);
+        else return launch_tile<AT, SF, 64, 64, 64, 32, 4, 3, !TWO_WAYS ? Order::AHEAD : Order::PLAIN>(p, s);
+    case 5: return launch_tile<AT, SF, 32, 64, 32, BYTES ? 16 : 32, 4, 3, Order::PLAIN>(p, s);
+    default: return launch_tile<AT, SF, 32, 32, 32, BYTES ? 16 : 32, 8, 3, Order::PLAIN>(p, s);
     }
 }
 

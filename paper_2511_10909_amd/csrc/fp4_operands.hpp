@@ -67,8 +67,21 @@ __device__ __forceinline__ Frag16 weights_fp16_by(uint32_t codes, f16x2 s)
     return f;
 }
 
-// eight FP16 activations, times 1 or 4, as sums of two BF16 numbers each (the weights of codes 253 and 254 reach 2^128: they are
-// taken at a quarter there, so that no infinity meets a zero of the smaller parts)
+// A quarter of the scale that an E8M0 code stands for (255: NaN).
+__device__ __forceinline__ float quarter_scale(uint32_t e8m0)
+{
+    return __uint_as_float(e8m0 == 255u ? 0x7FC00000u : e8m0 > 2u ? (e8m0 - 2u) << 23 : 0x00100000u << e8m0);
+}
+// FP16's second way: weights in BF16.  Those of codes 253 and 254 reach 2^128, and an infinity must not meet the zeros among the activations'
+// smaller parts.  Where a lane of the wavefront holds such a code (`far`, the same in all lanes: lane r holds weight row r and token r, and
+// an instruction multiplies each with all of the other), every lane takes its weights at a quarter, which is exact down to code 0, and its
+// activations four times.
+__device__ __forceinline__ bool any_far(uint32_t code) { return __any(code - 253u < 2u); }
+__device__ __forceinline__ Frag16 weights_second_way(uint32_t codes, uint32_t e8m0, bool far)
+{
+    return far ? weights_bf16_by(codes, quarter_scale(e8m0)) : weights_bf16(codes, e8m0);
+}
+// eight FP16 activations, times 1 or 4, as sums of two BF16 numbers each
 __device__ __forceinline__ void split_fp16(const Frag16 &x, float factor, Frag16 &hi, Frag16 &lo)
 {
 #pragma unroll

@@ -42,10 +42,10 @@ template <int AT, int SF> __device__ __forceinline__ f32x4 window_products(u32x4
             else acc = mfma_bf16(weights_bf16_by(w[j], (float)sj), Frag16{x[j]}, acc);
         }
     } else if (AT == MMAEMU_BF16 || !__all(fp16_holds(s))) {
-        const bool far = AT == MMAEMU_FP16 && s - 253u < 2u;
+        const bool far = AT == MMAEMU_FP16 && any_far(s);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const Frag16 f = weights_bf16(w[j], far ? s - 2 : s);
+            const Frag16 f = weights_second_way(w[j], s, far);
             if (AT == MMAEMU_FP16) {
                 Frag16 hi, lo;
                 split_fp16(Frag16{x[j]}, far ? 4.0f : 1.0f, hi, lo);

@@ -254,10 +254,10 @@ __global__ void __launch_bounds__((Tile<AT, SF, BM, BN, TM, TN, WK, S>::THREADS)
             } else if constexpr (AT == MMAEMU_FP16 && SF == MMAEMU_SCALE_FORMAT_E8M0) {
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    const bool far = q.ws[j] - 253u < 2u;
+                    const bool far = any_far(q.ws[j]);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const Frag16 f = weights_bf16(q.c[j][h], far ? q.ws[j] - 2 : q.ws[j]);
+                        const Frag16 f = weights_second_way(q.c[j][h], q.ws[j], far);
 #pragma unroll
                         for (int i = 0; i < MT; ++i) {
                             // (rare: one piece at a time in registers, and nothing kept of it for the next weights)

@@ -106,14 +106,24 @@ template <int T> __device__ __forceinline__ Raw8<T> round8(const float (&v)[8])
 }
 
 // Binary64 to binary32 such that a later rounding to a few bits comes out as if taken from the binary64 value: cut toward
-// zero, the last bit set where anything was lost.  (Values that are subnormal in binary32 are rounded there: they are
-// zeros to every caller.)
+// zero, the last bit set where anything was lost.  Values that are subnormal in binary32 are rounded there: zeros to E2M1, E4M3 and
+// FP16, but not to BF16, which reaches as far down.
 __device__ __forceinline__ float to_float_odd(double x)
 {
     uint64_t b = __builtin_bit_cast(uint64_t, x);
     const uint32_t low = (uint32_t)b & 0x1FFFFFFFu;
     b = (b & ~0x1FFFFFFFull) | (low ? 0x20000000ull : 0ull);
     return (float)__builtin_bit_cast(double, b);
+}
+
+// The same for all magnitudes: below binary32's least normal number its pattern counts units of 2^-149.
+__device__ __forceinline__ float to_float_odd_subnormal(double x)
+{
+    const double a = __builtin_fabs(x);
+    if (a >= 0x1p-126) return to_float_odd(x);
+    const double units = a * 0x1p149;              // exact, below 2^23
+    const uint32_t whole = (uint32_t)units;
+    return __builtin_copysignf(__uint_as_float(whole | ((double)whole != units ? 1u : 0u)), (float)x);
 }
 
 // ---- a block's E8M0 scale ---------------------------------------------------------------

@@ -109,10 +109,12 @@ __device__ __forceinline__ void quantize_vector(const QuantArgs &a, uint64_t row
             const f32x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),
                         p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3);
             const float e[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+            const bool low = T == MMAEMU_BF16 && a.tensor_scale < 0x1p-116f;           // (the least element and scale make 2^-10)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float es = e[i] * scale;                         // exact: 2 + 4 bits, and 24 more with the tensor's scale
-                out[i] = T == MMAEMU_FP32 ? es * a.tensor_scale : to_float_odd((double)es * (double)a.tensor_scale);
+                const double v = (double)es * (double)a.tensor_scale;
+                out[i] = T == MMAEMU_FP32 ? es * a.tensor_scale : low ? to_float_odd_subnormal(v) : to_float_odd(v);
                 if (nan) out[i] = __uint_as_float(0x7FC00000u);
             }
         }

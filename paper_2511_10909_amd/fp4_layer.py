@@ -13,9 +13,21 @@ from . import binding as mm
 from . import presets
 
 
+def _row_stride(t, what):
+    """Elements from one row of t to the next, as the operators count them."""
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("%s: a row's elements must follow one another, not be %d apart" % (what, t.stride(1)))
+    stride = t.stride(0) if rows > 1 else cols
+    if stride < cols:
+        raise ValueError("%s: rows of %d elements, %d apart" % (what, cols, stride))
+    return stride
+
+
 class Fp4Layer:
     """x, residual -> W norm(x + residual), residual <- x + residual, for at most `tokens` tokens at a time.  W[n][k] (k a multiple of 32) and the
-    norm's weights in BF16 or FP16; W is kept in MXFP4 with scales under which nothing saturates."""
+    norm's weights in BF16 or FP16; W is kept in MXFP4 with scales under which nothing saturates.  Rows of x, the residual and the output may be
+    slices of wider ones."""
 
     def __init__(self, W, norm_weight, tokens, code=mm.E4M3, eps=1e-6):
         self.n, self.k = W.shape
@@ -33,8 +45,11 @@ class Fp4Layer:
         m = x.shape[0]
         if m > self.A.shape[0]:
             raise ValueError("%d tokens in a layer made for %d" % (m, self.A.shape[0]))
-        mm.rmsnorm_quantize(x, residual, self.norm_weight, residual, self.A, self.SA, m, self.k, self.type, self.type, self.code, mm.SCALE_RULE_FLOOR, self.eps)
-        mm.matmul_fp4(self.A, self.SA, self.W, self.SW, out, m, self.n, self.k, self.code, self.type)
+        x_stride, out_stride = _row_stride(x, "x"), _row_stride(out, "out")
+        residual_stride = 0 if residual is None else _row_stride(residual, "residual")
+        mm.rmsnorm_quantize(x, residual, self.norm_weight, residual, self.A, self.SA, m, self.k, self.type, self.type, self.code, mm.SCALE_RULE_FLOOR, self.eps,
+                            x_stride, residual_stride)
+        mm.matmul_fp4(self.A, self.SA, self.W, self.SW, out, m, self.n, self.k, self.code, self.type, d_stride=out_stride)
         return out
 
 

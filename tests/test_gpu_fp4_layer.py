@@ -1,0 +1,33 @@
+"""A layer on FP4 weights: slices of wider buffers give what contiguous tensors give, and nothing beside them is written."""
+import pytest
+import torch
+
+from paper_2511_10909_amd import fp4_layer
+
+pytestmark = pytest.mark.gpu
+
+
+def normal(*shape, seed=0, dtype=torch.bfloat16):
+    return torch.randn(shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)).to(dtype)
+
+
+def slice_of(t, stride, fill=-7.0):
+    """t's values as a slice of a wider buffer, and the buffer."""
+    wide = torch.full((t.shape[0], stride), fill, dtype=t.dtype, device=t.device)
+    wide[:, :t.shape[1]] = t
+    return wide[:, :t.shape[1]], wide
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m", [1, 2, 16, 40])
+def test_slices_of_wider_buffers(m, dtype):
+    n, k = 200, 320
+    layer = fp4_layer.Fp4Layer(normal(n, k, dtype=dtype), normal(k, seed=1, dtype=dtype), 40)
+    x, residual = normal(m, k, seed=2, dtype=dtype), normal(m, k, seed=3, dtype=dtype)
+    r, out = residual.clone(), torch.empty((m, n), dtype=dtype, device="cuda")
+    layer(x, r, out)
+    (xs, _), (rs, rw), (os, ow) = slice_of(x, k + 3), slice_of(residual, k + 32), slice_of(torch.zeros_like(out), n + 1)
+    layer(xs, rs, os)
+    assert torch.equal(os, out) and torch.equal(rs, r)
+    assert bool((rw[:, k:] == -7.0).all()) and bool((ow[:, n:] == -7.0).all())
+    assert torch.equal(r, (x.float() + residual.float()).to(dtype))

@@ -65,3 +65,60 @@ def test_rows_that_are_not_rows_are_refused(calls, which, how):
     with pytest.raises(ValueError):
         layer(*tensors)
     assert not calls
+
+
+@pytest.mark.parametrize("which,shape", [(0, (5, 63)), (0, (5, 65)), (0, (5,)), (0, (1, 5, 64)), (0, (9, 64)), (1, (4, 64)), (1, (5, 32)), (1, (64,)), (2, (4, 48)), (2, (5, 47)),
+                                         (2, (5, 64)), (2, (48,)), (2, (1, 5, 48))])
+def test_other_sizes_are_refused(calls, which, shape):
+    """A layer of 64 inputs and 48 outputs for eight tokens: anything else would be read or written beyond its end."""
+    layer = layer_of()
+    tensors = [torch.zeros(s, dtype=BF16) for s in ((5, 64), (5, 64), (5, 48))]
+    tensors[which] = torch.zeros(shape, dtype=BF16)
+    del calls[:]
+    with pytest.raises(ValueError):
+        layer(*tensors)
+    assert not calls
+
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_tensors_elsewhere_are_refused(calls, which):
+    layer = layer_of()
+    tensors = [torch.zeros(s, dtype=BF16) for s in ((5, 64), (5, 64), (5, 48))]
+    tensors[which] = tensors[which].to("meta")
+    del calls[:]
+    with pytest.raises(ValueError):
+        layer(*tensors)
+    assert not calls
+
+
+@pytest.mark.parametrize("W,norm_weight", [((64,), (64,)), ((2, 48, 64), (64,)), ((48, 64), (63,)), ((48, 64), (65,)), ((48, 64), (48, 64)), ((0, 64), (64,)), ((48, 0), (0,))])
+def test_weights_of_other_sizes_are_refused(calls, W, norm_weight):
+    with pytest.raises(ValueError):
+        fp4_layer.Fp4Layer(torch.zeros(W, dtype=BF16), torch.zeros(norm_weight, dtype=BF16), 8)
+    assert not calls
+
+
+def test_norm_weights_elsewhere_are_refused(calls):
+    with pytest.raises(ValueError):
+        fp4_layer.Fp4Layer(torch.zeros((48, 64), dtype=BF16), torch.zeros(64, dtype=BF16, device="meta"), 8)
+    assert not calls
+
+
+def test_a_residual_and_an_output_of_more_rows(calls):
+    layer = layer_of()
+    residual, out = wide(7, 64, 80), wide(8, 48, 48)
+    del calls[:]
+    assert layer(wide(5, 64, 64), residual, out) is out
+    assert calls[0][1]["rows"] == 5 and calls[0][1]["residual_stride"] == 80 and calls[1][1]["m"] == 5
+    del calls[:]
+    layer(wide(1, 64, 64), residual, out)
+    assert calls[0][1]["rows"] == 1 and calls[1][1]["m"] == 1
+
+
+def test_no_residual_and_no_tokens(calls):
+    layer = fp4_layer.Fp4Layer(torch.zeros((48, 64), dtype=BF16), None, 8)
+    del calls[:]
+    layer(torch.zeros((3, 64), dtype=BF16), None, torch.zeros((3, 48), dtype=BF16))
+    layer(torch.zeros((0, 64), dtype=BF16), torch.zeros((0, 64), dtype=BF16), torch.zeros((0, 48), dtype=BF16))
+    assert [(a.get("rows"), a.get("m")) for _, a in calls] == [(3, None), (None, 3), (0, None), (None, 0)]
+    assert calls[0][1]["weight"] is None and calls[0][1]["residual"] is None and calls[0][1]["residual_out"] is None

@@ -13,10 +13,14 @@ from . import binding as mm
 from . import presets
 
 
-def _row_stride(t, what, rows, cols, device):
+_TYPES = {torch.bfloat16: mm.BF16, torch.float16: mm.FP16}
+
+
+def _row_stride(t, what, rows, cols, dtype, device):
     """Elements from one row of t to the next, as the operators count them, for a tensor of at least `rows` rows of `cols` elements."""
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or t.device != device:
-        raise ValueError("%s: %d rows of %d elements on %s are asked for, not %s on %s" % (what, rows, cols, device, tuple(t.shape), t.device))
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or t.dtype != dtype or t.device != device:
+        raise ValueError("%s: %d rows of %d elements in %s on %s are asked for, not %s in %s on %s" %
+                         (what, rows, cols, dtype, device, tuple(t.shape), t.dtype, t.device))
     if cols > 1 and t.stride(1) != 1:
         raise ValueError("%s: a row's elements must follow one another, not be %d apart" % (what, t.stride(1)))
     stride = t.stride(0) if rows > 1 else cols
@@ -26,9 +30,10 @@ def _row_stride(t, what, rows, cols, device):
 
 
 class Fp4Layer:
-    """x, residual -> W norm(x + residual), residual <- x + residual, for at most `tokens` tokens at a time.  W[n][k] (k a multiple of 32) and the
-    norm's weights (None: ones) in BF16 or FP16; W is kept in MXFP4 with scales under which nothing saturates.  x[m][k], the residual (None: no
-    residual stream) and the output may have rows that are slices of wider ones, and the latter two more rows than x, which stay as they are."""
+    """x, residual -> W norm(x + residual), residual <- x + residual, for at most `tokens` tokens at a time.  W[n][k] (k a multiple of 32) in BF16 or FP16
+    is kept in MXFP4 with scales under which nothing saturates; the norm's weights (None: ones) have W's type or are binary32.  x[m][k], the residual
+    (None: no residual stream) and the output have W's type; their rows may be slices of wider ones, and the latter two may have more rows than x,
+    which stay as they are."""
 
     def __init__(self, W, norm_weight, tokens, code=mm.E4M3, eps=1e-6):
         if W.dim() != 2 or 0 in W.shape:
@@ -38,7 +43,10 @@ class Fp4Layer:
             raise ValueError("a layer's inputs come in multiples of 32, not %d" % self.k)
         if norm_weight is not None and (norm_weight.numel() != self.k or norm_weight.device != W.device):
             raise ValueError("the norm's weights: %d on %s are asked for, not %s on %s" % (self.k, W.device, tuple(norm_weight.shape), norm_weight.device))
-        self.type = {torch.bfloat16: mm.BF16, torch.float16: mm.FP16}[W.dtype]
+        if W.dtype not in _TYPES or (norm_weight is not None and norm_weight.dtype not in (W.dtype, torch.float32)):
+            raise ValueError("a layer's weights are BF16 or FP16, the norm's the same or binary32")
+        self.dtype, self.type = W.dtype, _TYPES[W.dtype]
+        self.norm_type = mm.FP32 if norm_weight is not None and norm_weight.dtype == torch.float32 else self.type
         self.norm_weight, self.code, self.eps = norm_weight, code, eps
         self.W = torch.empty((self.n, self.k // 2), dtype=torch.uint8, device=W.device)
         self.SW = torch.empty((self.n, self.k // 32), dtype=torch.uint8, device=W.device)
@@ -50,10 +58,10 @@ class Fp4Layer:
         m = x.shape[0]
         if m > self.A.shape[0]:
             raise ValueError("%d tokens in a layer made for %d" % (m, self.A.shape[0]))
-        device = self.W.device
-        x_stride, out_stride = _row_stride(x, "x", m, self.k, device), _row_stride(out, "out", m, self.n, device)
-        residual_stride = 0 if residual is None else _row_stride(residual, "residual", m, self.k, device)
-        mm.rmsnorm_quantize(x, residual, self.norm_weight, residual, self.A, self.SA, m, self.k, self.type, self.type, self.code, mm.SCALE_RULE_FLOOR, self.eps,
+        kind = self.dtype, self.W.device
+        x_stride, out_stride = _row_stride(x, "x", m, self.k, *kind), _row_stride(out, "out", m, self.n, *kind)
+        residual_stride = 0 if residual is None else _row_stride(residual, "residual", m, self.k, *kind)
+        mm.rmsnorm_quantize(x, residual, self.norm_weight, residual, self.A, self.SA, m, self.k, self.type, self.norm_type, self.code, mm.SCALE_RULE_FLOOR, self.eps,
                             x_stride, residual_stride)
         mm.matmul_fp4(self.A, self.SA, self.W, self.SW, out, m, self.n, self.k, self.code, self.type, d_stride=out_stride)
         return out

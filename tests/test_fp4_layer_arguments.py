@@ -122,3 +122,35 @@ def test_no_residual_and_no_tokens(calls):
     layer(torch.zeros((0, 64), dtype=BF16), torch.zeros((0, 64), dtype=BF16), torch.zeros((0, 48), dtype=BF16))
     assert [(a.get("rows"), a.get("m")) for _, a in calls] == [(3, None), (None, 3), (0, None), (None, 0)]
     assert calls[0][1]["weight"] is None and calls[0][1]["residual"] is None and calls[0][1]["residual_out"] is None
+
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32, torch.uint8])
+def test_tensors_of_another_type_are_refused(calls, which, dtype):
+    layer = layer_of()
+    tensors = [torch.zeros(s, dtype=BF16) for s in ((5, 64), (5, 64), (5, 48))]
+    tensors[which] = tensors[which].to(dtype)
+    del calls[:]
+    with pytest.raises(ValueError):
+        layer(*tensors)
+    assert not calls
+
+
+@pytest.mark.parametrize("dtype,known", [(BF16, "BF16"), (torch.float16, "FP16")])
+def test_norm_weights_in_binary32_or_in_the_layers_type(calls, dtype, known):
+    mm = fp4_layer.mm
+    for norm_weight, want in ((torch.zeros(64, dtype=dtype), getattr(mm, known)), (torch.zeros(64), mm.FP32), (None, getattr(mm, known))):
+        layer = fp4_layer.Fp4Layer(torch.zeros((48, 64), dtype=dtype), norm_weight, 8)
+        del calls[:]
+        layer(*(torch.zeros(s, dtype=dtype) for s in ((5, 64), (5, 64), (5, 48))))
+        assert (calls[0][1]["type"], calls[0][1]["weight_type"]) == (getattr(mm, known), want)
+    for other in (torch.float16 if dtype == BF16 else BF16, torch.float64, torch.int16):
+        with pytest.raises(ValueError):
+            fp4_layer.Fp4Layer(torch.zeros((48, 64), dtype=dtype), torch.zeros(64).to(other), 8)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float64, torch.uint8])
+def test_weights_of_other_types_are_refused(calls, dtype):
+    with pytest.raises((ValueError, KeyError)):
+        fp4_layer.Fp4Layer(torch.zeros((48, 64), dtype=dtype), torch.zeros(64, dtype=dtype), 8)
+    assert not calls

@@ -31,3 +31,15 @@ def test_slices_of_wider_buffers(m, dtype):
     assert torch.equal(os, out) and torch.equal(rs, r)
     assert bool((rw[:, k:] == -7.0).all()) and bool((ow[:, n:] == -7.0).all())
     assert torch.equal(r, (x.float() + residual.float()).to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_norm_weights_in_binary32(dtype):
+    """Binary32 weights of values that the layer's type holds give what the same values in that type give."""
+    n, k, m = 96, 160, 5
+    W, w = normal(n, k, dtype=dtype), normal(k, seed=1, dtype=dtype)
+    outs = []
+    for norm_weight in (w, w.float()):
+        x, residual, out = normal(m, k, seed=2, dtype=dtype), normal(m, k, seed=3, dtype=dtype), torch.empty((m, n), dtype=dtype, device="cuda")
+        outs.append(fp4_layer.Fp4Layer(W, norm_weight, m)(x, residual, out))
+    assert torch.equal(*outs)

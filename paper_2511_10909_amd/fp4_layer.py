@@ -31,9 +31,9 @@ def _row_stride(t, what, rows, cols, dtype, device):
 
 class Fp4Layer:
     """x, residual -> W norm(x + residual), residual <- x + residual, for at most `tokens` tokens at a time.  W[n][k] (k a multiple of 32) in BF16 or FP16
-    is kept in MXFP4 with scales under which nothing saturates; the norm's weights (None: ones) have W's type or are binary32.  x[m][k], the residual
-    (None: no residual stream) and the output have W's type; their rows may be slices of wider ones, and the latter two may have more rows than x,
-    which stay as they are."""
+    is kept in MXFP4 with scales under which nothing saturates; the norm's weights (None: ones) have W's type or are binary32; both may lie in any
+    layout.  x[m][k], the residual (None: no residual stream) and the output have W's type; their rows may be slices of wider ones, and the latter
+    two may have more rows than x, which stay as they are."""
 
     def __init__(self, W, norm_weight, tokens, code=mm.E4M3, eps=1e-6):
         if W.dim() != 2 or 0 in W.shape:
@@ -47,12 +47,16 @@ class Fp4Layer:
             raise ValueError("a layer's weights are BF16 or FP16, the norm's the same or binary32")
         self.dtype, self.type = W.dtype, _TYPES[W.dtype]
         self.norm_type = mm.FP32 if norm_weight is not None and norm_weight.dtype == torch.float32 else self.type
-        self.norm_weight, self.code, self.eps = norm_weight, code, eps
+        if (W.stride(1) != 1 and self.k > 1) or (W.stride(0) < self.k and self.n > 1):
+            W = W.contiguous()
+        self.norm_weight = norm_weight if norm_weight is None else norm_weight.contiguous()
+        self.code, self.eps = code, eps
         self.W = torch.empty((self.n, self.k // 2), dtype=torch.uint8, device=W.device)
         self.SW = torch.empty((self.n, self.k // 32), dtype=torch.uint8, device=W.device)
         self.A = torch.empty((tokens, self.k), dtype=torch.uint8, device=W.device)
         self.SA = torch.empty((tokens, self.k // 32), dtype=torch.uint8, device=W.device)
-        mm.quantize_fp4(W, self.W, self.SW, None, self.n, self.k, self.type, mm.SCALE_FORMAT_E8M0, mm.SCALE_RULE_FIT, x_stride=W.stride(0))
+        mm.quantize_fp4(W, self.W, self.SW, None, self.n, self.k, self.type, mm.SCALE_FORMAT_E8M0, mm.SCALE_RULE_FIT,
+                        x_stride=W.stride(0) if self.n > 1 else self.k)
 
     def __call__(self, x, residual, out):
         m = x.shape[0]

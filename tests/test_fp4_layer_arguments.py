@@ -154,3 +154,33 @@ def test_weights_of_other_types_are_refused(calls, dtype):
     with pytest.raises((ValueError, KeyError)):
         fp4_layer.Fp4Layer(torch.zeros((48, 64), dtype=dtype), torch.zeros(64, dtype=dtype), 8)
     assert not calls
+
+
+@pytest.mark.parametrize("how", ["rows of a wider one", "every other column", "transposed", "one row for all", "one row", "every other row"])
+def test_weights_in_any_layout(calls, how):
+    """What is quantised are the weights that were given: through the stride of their rows, or as a copy."""
+    base = torch.arange(96 * 128).reshape(96, 128).to(BF16)
+    W = {"rows of a wider one": base[:, 8:72], "every other column": base[:, ::2], "transposed": base[:64, :48].t(), "one row for all": base[:1, :64].expand(48, 64),
+         "one row": base[:, :64].as_strided((1, 64), (5, 1)), "every other row": base[::2, :64]}[how]
+    layer = fp4_layer.Fp4Layer(W, None, 8)
+    (_, a), = calls
+    assert (a["rows"], a["cols"]) == tuple(W.shape) == (layer.n, layer.k)
+    seen = torch.as_strided(a["x"], W.shape, (a["x_stride"], 1), a["x"].storage_offset())
+    assert a["x_stride"] >= 64 and torch.equal(seen, W)
+    if how in ("rows of a wider one", "every other row"):
+        assert a["x"] is W                                             # (no copy where the operator takes the layout)
+
+
+@pytest.mark.parametrize("how", ["every other element", "one for all", "a column"])
+def test_norm_weights_in_any_layout(calls, how):
+    w = {"every other element": torch.arange(128.0)[::2], "one for all": torch.full((1,), 3.0).expand(64), "a column": torch.arange(128.0).reshape(64, 2)[:, 1]}[how]
+    layer = fp4_layer.Fp4Layer(torch.zeros((48, 64), dtype=BF16), w, 8)
+    del calls[:]
+    layer(*(torch.zeros(s, dtype=BF16) for s in ((5, 64), (5, 64), (5, 48))))
+    passed = calls[0][1]["weight"]
+    assert passed.is_contiguous() and torch.equal(passed, w)
+
+
+def test_norm_weights_that_lie_as_the_operator_wants_are_not_copied(calls):
+    w = torch.ones(64, dtype=BF16)
+    assert fp4_layer.Fp4Layer(torch.zeros((48, 64), dtype=BF16), w, 8).norm_weight is w

@@ -18,22 +18,26 @@ _TYPES = {torch.bfloat16: mm.BF16, torch.float16: mm.FP16}
 
 def _row_stride(t, what, rows, cols, dtype, device):
     """Elements from one row of t to the next, as the operators count them, for a tensor of at least `rows` rows of `cols` elements."""
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or t.dtype != dtype or t.device != device:
+    shape = t.shape
+    if len(shape) != 2 or shape[0] < rows or shape[1] != cols or t.dtype != dtype or t.device != device:
         raise ValueError("%s: %d rows of %d elements in %s on %s are asked for, not %s in %s on %s" %
-                         (what, rows, cols, dtype, device, tuple(t.shape), t.dtype, t.device))
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError("%s: a row's elements must follow one another, not be %d apart" % (what, t.stride(1)))
-    stride = t.stride(0) if rows > 1 else cols
-    if stride < cols:
-        raise ValueError("%s: rows of %d elements, %d apart" % (what, cols, stride))
-    return stride
+                         (what, rows, cols, dtype, device, tuple(shape), t.dtype, t.device))
+    apart, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError("%s: a row's elements must follow one another, not be %d apart" % (what, step))
+    if rows <= 1:
+        return cols
+    if apart < cols:
+        raise ValueError("%s: rows of %d elements, %d apart" % (what, cols, apart))
+    return apart
 
 
 class Fp4Layer:
     """x, residual -> W norm(x + residual), residual <- x + residual, for at most `tokens` tokens at a time.  W[n][k] (k a multiple of 32) in BF16 or FP16
     is kept in MXFP4 with scales under which nothing saturates; the norm's weights (None: ones) have W's type or are binary32; both may lie in any
     layout.  x[m][k], the residual (None: no residual stream) and the output have W's type; their rows may be slices of wider ones, and the latter
-    two may have more rows than x, which stay as they are."""
+    two may have more rows than x, which stay as they are.  Every call has its activations' codes and scales in memory of its own, taken on the
+    stream (or in the capture) that it is made on: calls on several streams may run at once."""
 
     def __init__(self, W, norm_weight, tokens, code=mm.E4M3, eps=1e-6):
         if W.dim() != 2 or 0 in W.shape:
@@ -45,7 +49,7 @@ class Fp4Layer:
             raise ValueError("the norm's weights: %d on %s are asked for, not %s on %s" % (self.k, W.device, tuple(norm_weight.shape), norm_weight.device))
         if W.dtype not in _TYPES or (norm_weight is not None and norm_weight.dtype not in (W.dtype, torch.float32)):
             raise ValueError("a layer's weights are BF16 or FP16, the norm's the same or binary32")
-        self.dtype, self.type = W.dtype, _TYPES[W.dtype]
+        self.device, self.dtype, self.type = W.device, W.dtype, _TYPES[W.dtype]
         self.norm_type = mm.FP32 if norm_weight is not None and norm_weight.dtype == torch.float32 else self.type
         if (W.stride(1) != 1 and self.k > 1) or (W.stride(0) < self.k and self.n > 1):
             W = W.contiguous()
@@ -53,21 +57,35 @@ class Fp4Layer:
         self.code, self.eps = code, eps
         self.W = torch.empty((self.n, self.k // 2), dtype=torch.uint8, device=W.device)
         self.SW = torch.empty((self.n, self.k // 32), dtype=torch.uint8, device=W.device)
-        self.A = torch.empty((tokens, self.k), dtype=torch.uint8, device=W.device)
-        self.SA = torch.empty((tokens, self.k // 32), dtype=torch.uint8, device=W.device)
+        self.tokens = tokens
         mm.quantize_fp4(W, self.W, self.SW, None, self.n, self.k, self.type, mm.SCALE_FORMAT_E8M0, mm.SCALE_RULE_FIT,
                         x_stride=W.stride(0) if self.n > 1 else self.k)
 
-    def __call__(self, x, residual, out):
-        m = x.shape[0]
-        if m > self.A.shape[0]:
-            raise ValueError("%d tokens in a layer made for %d" % (m, self.A.shape[0]))
-        kind = self.dtype, self.W.device
-        x_stride, out_stride = _row_stride(x, "x", m, self.k, *kind), _row_stride(out, "out", m, self.n, *kind)
-        residual_stride = 0 if residual is None else _row_stride(residual, "residual", m, self.k, *kind)
-        mm.rmsnorm_quantize(x, residual, self.norm_weight, residual, self.A, self.SA, m, self.k, self.type, self.norm_type, self.code, mm.SCALE_RULE_FLOOR, self.eps,
+    def _norm(self, x, residual, m):
+        """The codes' memory, m k bytes and m k / 32 of scales after them, with the norm on its way into it."""
+        if m > self.tokens:
+            raise ValueError("%d tokens in a layer made for %d" % (m, self.tokens))
+        k = self.k
+        x_stride = _row_stride(x, "x", m, k, self.dtype, self.device)
+        residual_stride = 0 if residual is None else _row_stride(residual, "residual", m, k, self.dtype, self.device)
+        memory = torch.empty(m * k + m * k // 32, dtype=torch.uint8, device=self.device)
+        at = memory.data_ptr()
+        mm.rmsnorm_quantize(x, residual, self.norm_weight, residual, at, at + m * k, m, k, self.type, self.norm_type, self.code, mm.SCALE_RULE_FLOOR, self.eps,
                             x_stride, residual_stride)
-        mm.matmul_fp4(self.A, self.SA, self.W, self.SW, out, m, self.n, self.k, self.code, self.type, d_stride=out_stride)
+        return memory
+
+    def activations(self, x, residual):
+        """norm(x + residual) as codes [m][k] and scales [m][k / 32]; residual <- x + residual."""
+        m = x.shape[0]
+        codes, scales = self._norm(x, residual, m).split((m * self.k, m * self.k // 32))
+        return codes.view(m, self.k), scales.view(m, self.k // 32)
+
+    def __call__(self, x, residual, out):
+        m, k = x.shape[0], self.k
+        out_stride = _row_stride(out, "out", m, self.n, self.dtype, self.device)
+        memory = self._norm(x, residual, m)
+        at = memory.data_ptr()
+        mm.matmul_fp4(at, at + m * k, self.W, self.SW, out, m, self.n, k, self.code, self.type, d_stride=out_stride)
         return out
 
 
@@ -110,7 +128,7 @@ def run_stack(layers=4, width=4096, prompt=2048, generated=32, seed=0, dev="cuda
     first = stack[0](x, residual.clone(), outs[0])[:8].double()
     want = (h / torch.sqrt(h.square().mean(1, keepdim=True) + 1e-6)) @ weights[0].double().t()
     error = ((first - want).norm() / want.norm()).item()
-    mismatches, compared = model_mismatches(stack[0].A, stack[0].SA, stack[0].W, stack[0].SW, prompt, width, width)
+    mismatches, compared = model_mismatches(*stack[0].activations(x, residual.clone()), stack[0].W, stack[0].SW, prompt, width, width)
 
     forward(x, residual, outs)
     torch.cuda.synchronize()

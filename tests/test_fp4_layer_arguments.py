@@ -184,3 +184,25 @@ def test_norm_weights_in_any_layout(calls, how):
 def test_norm_weights_that_lie_as_the_operator_wants_are_not_copied(calls):
     w = torch.ones(64, dtype=BF16)
     assert fp4_layer.Fp4Layer(torch.zeros((48, 64), dtype=BF16), w, 8).norm_weight is w
+
+
+def test_calls_share_no_memory(calls, monkeypatch):
+    """Two calls' codes and scales lie apart, as calls on two streams need, each within memory taken for its call."""
+    layer = layer_of()
+    taken = []
+
+    def empty(*args, **kw):
+        taken.append(torch.zeros(*args, **{k: v for k, v in kw.items() if k != "device"}))
+        return taken[-1]
+
+    monkeypatch.setattr(fp4_layer.torch, "empty", empty)
+    del calls[:]
+    tokens = 5, 5, 1
+    for m in tokens:
+        layer(*(torch.zeros(s, dtype=BF16) for s in ((m, 64), (m, 64), (m, 48))))
+    assert len(taken) == 3
+    for m, memory, (_, a), (_, b) in zip(tokens, taken, calls[0::2], calls[1::2]):
+        at = memory.data_ptr()
+        codes, scales = a["codes"], a["scales"]
+        assert (b["A"], b["SA"]) == (codes, scales) and codes % 16 == 0
+        assert at <= codes and codes + 64 * m <= scales and scales + 2 * m <= at + memory.numel() * memory.element_size()

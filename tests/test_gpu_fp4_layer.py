@@ -43,3 +43,31 @@ def test_norm_weights_in_binary32(dtype):
         x, residual, out = normal(m, k, seed=2, dtype=dtype), normal(m, k, seed=3, dtype=dtype), torch.empty((m, n), dtype=dtype, device="cuda")
         outs.append(fp4_layer.Fp4Layer(W, norm_weight, m)(x, residual, out))
     assert torch.equal(*outs)
+
+
+def test_a_prompt_on_one_stream_and_tokens_from_a_graph_on_another():
+    """Each keeps its own codes: the outputs are those of the same calls one after the other."""
+    n = k = 2048
+    m, prompts, tokens = 512, 6, 40
+    layer = fp4_layer.Fp4Layer(normal(n, k), normal(k, seed=1), m)
+    xs = [normal(m, k, seed=10 + i) for i in range(prompts)]
+    token, want_token = normal(1, k, seed=5), torch.empty((1, n), dtype=torch.bfloat16, device="cuda")
+    layer(token, None, want_token)
+    want = [layer(x, None, torch.empty((m, n), dtype=torch.bfloat16, device="cuda")) for x in xs]
+    torch.cuda.synchronize()
+    one, other, graph = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    token_out, seen = torch.empty_like(want_token), torch.empty((tokens, n), dtype=torch.bfloat16, device="cuda")
+    with torch.cuda.graph(graph, stream=other):
+        layer(token, None, token_out)
+    outs = [torch.empty((m, n), dtype=torch.bfloat16, device="cuda") for _ in xs]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(one):
+        for x, out in zip(xs, outs):
+            layer(x, None, out)
+    with torch.cuda.stream(other):
+        for i in range(tokens):
+            graph.replay()
+            seen[i].copy_(token_out[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    assert torch.equal(seen, want_token.expand_as(seen))

@@ -92,7 +92,8 @@ class Fp4Layer:
 def model_mismatches(A, SA, W, SW, m, n, k, code=mm.E4M3):
     """Outputs of matmul_fp4 (binary32) that differ from the model of v_mfma_scale_f32_16x16x128_f8f6f4 on the same operands, bit for bit, and the
     number of outputs.  The model adds all k products in one chain, as the kernels do whose wavefronts split no sums: those in blocks of
-    128 x 256 and 256 x 256, and any kernel for k up to 128."""
+    128 x 256 and 256 x 256, and any kernel for k up to 128.  The others (few tokens, smaller blocks, and the smaller blocks that finish a product in
+    two launches) add their wavefronts' chains in binary32, and differ in the last bits."""
     D, Dm, C = (torch.zeros((m, n), dtype=torch.float32, device=A.device) for _ in range(3))
     mm.matmul_fp4(A, SA, W, SW, D, m, n, k, code, mm.FP32)
     one_a_byte = torch.stack((W & 15, W >> 4), dim=-1).reshape(n, k)
@@ -157,7 +158,14 @@ def run_stack(layers=4, width=4096, prompt=2048, generated=32, seed=0, dev="cuda
     torch.cuda.synchronize()
     token_s = (time.perf_counter() - t0) / generated
     return dict(prompt_seconds=prompt_s, prompt_flops=2 * layers * prompt * width * width, token_seconds=token_s, relative_error=error,
-                mismatches=mismatches, compared=compared, finite=bool(torch.isfinite(last).all()))
+                mismatches=mismatches, compared=compared, kernel=mm.matmul_fp4_kernel(prompt, width, width, stack[0].code), finite=bool(torch.isfinite(last).all()))
+
+
+def _model_line(mismatches, compared, kernel):
+    line = "first layer's product (%s) against the model of the scaled instruction: %d of %d outputs differ" % (kernel, mismatches, compared)
+    if mismatches:
+        line += "; the model adds a row's products in one chain, blocks below 128 x 256 in several: last bits differ there"
+    return line
 
 
 def _report(argv=None):
@@ -173,7 +181,7 @@ def _report(argv=None):
                                                                                    r["prompt_flops"] / r["prompt_seconds"] / 1e12))
     print("a token: %.1f us (two launches per layer, replayed from a graph)" % (1e6 * r["token_seconds"]))
     print("first layer against its BF16 weights: relative error %.4f" % r["relative_error"])
-    print("first layer's product against the model of the scaled instruction: %d of %d outputs differ" % (r["mismatches"], r["compared"]))
+    print(_model_line(r["mismatches"], r["compared"], r["kernel"]))
 
 
 if __name__ == "__main__":

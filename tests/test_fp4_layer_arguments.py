@@ -206,3 +206,9 @@ def test_calls_share_no_memory(calls, monkeypatch):
         codes, scales = a["codes"], a["scales"]
         assert (b["A"], b["SA"]) == (codes, scales) and codes % 16 == 0
         assert at <= codes and codes + 64 * m <= scales and scales + 2 * m <= at + memory.numel() * memory.element_size()
+
+
+def test_the_report_says_where_differing_outputs_are_expected():
+    same, differ = fp4_layer._model_line(0, 400, "blocks of 256 x 256"), fp4_layer._model_line(7, 400, "blocks of 32 x 64")
+    assert "0 of 400" in same and "256 x 256" in same and "chain" not in same
+    assert "7 of 400" in differ and "blocks of 32 x 64" in differ and "one chain" in differ and "last bits differ" in differ

@@ -877,7 +877,7 @@ mmaemu_status mmaemu_rmsnorm_quantize(const void *x, const void *residual, const
     if (residual_stride == 0) residual_stride = cols;
     if (cols == 0 || cols > (1u << 24)) { set_error("rmsnorm_quantize: cols=%u outside 1 .. 2^24", cols); return MMAEMU_ERR_SHAPE; }
     const uint64_t widest = x_stride > residual_stride ? x_stride : residual_stride;
-    if (x_stride < cols || residual_stride < cols || widest >= (1ull << 48) || rows > (1ull << 48) / widest) {
+    if (x_stride < cols || residual_stride < cols || widest >= (1ull << 48) || rows > ((1ull << 48) - 1) / widest) {
         set_error("rmsnorm_quantize: a stride below cols, or rows * stride of 2^48 and more");
         return MMAEMU_ERR_SHAPE;
     }
@@ -906,7 +906,7 @@ mmaemu_status mmaemu_quantize_fp4(const void *x, void *codes, void *scales, void
     }
     if (x_stride == 0) x_stride = cols;
     if (cols == 0 || cols > (1u << 24)) { set_error("quantize_fp4: cols=%u outside 1 .. 2^24", cols); return MMAEMU_ERR_SHAPE; }
-    if (x_stride < cols || x_stride >= (1ull << 48) || rows > (1ull << 48) / x_stride) {
+    if (x_stride < cols || x_stride >= (1ull << 48) || rows > ((1ull << 48) - 1) / x_stride) {
         set_error("quantize_fp4: x_stride below cols, or rows * x_stride of 2^48 and more");
         return MMAEMU_ERR_SHAPE;
     }

@@ -215,9 +215,15 @@ constexpr uint32_t STREAM_TOKENS = 16;
 //   7 tokens, 8192 x 8192: 16 rows x 2 windows 7.8 and 8.7, 32 x 2 8.1 and 10.0;  13824 x 3776: 16 x 2 12.1 and 13.1, 16 x 1 10.3 and 10.3,
 //     32 x 2 10.3 and 11.4;  20000 x 5120: 16 x 1 14.0 and 13.7, 32 x 2 18.7 and 16.2;  12864 x 8192: 16 x 1 13.2 and 15.1, 32 x 2 11.5 and 13.5
 //   14 tokens, 7552 x 3904: 16 x 1 8.6 and 8.1, 32 x 1 9.3 and 9.1;  8192 x 8192: 32 x 2 9.1 and 11.0, 32 x 1 9.8 and 10.7, 32 x 1 of eight
-//     wavefronts 10.3 and 10.2;  13824 x 3776: 32 x 1 12.1 and 11.7, 64 x 1 14.0 and 14.4;  28672 x 8192: 64 x 1 34 and 38, 32 x 1 37 and 39;
-//     20000 x 5120 (a few more workgroups than 64 rows each leave resident): 64 x 1 28 and 24, 16 x 1 20 and 17
-// 8-bit ones: 14 tokens, 7552 x 3904: 16 x 2 7.9, 32 x 2 8.6;  13824 x 3776: 12.9 and 10.1;  20000 x 5120: 32 x 2 18.4, 32 x 1 14.2;  28672 x 8192: 27 and 31
+//     wavefronts 10.3 and 10.2;  13824 x 3776: 32 x 1 12.1 and 11.7, 64 x 1 14.0 and 14.4
+// 8-bit ones: 14 tokens, 7552 x 3904: 16 x 2 7.9, 32 x 2 8.6;  13824 x 3776: 12.9 and 10.1
+// Beyond 8192 weight rows: fifteen numbers of them up to 131072, rows of 1024 to 16384 products, 6 to 16 tokens.  The time of what is taken, over that
+// of the fastest of these shapes: 1.02 to 1.07 in the mean of a kind and number of tokens, at most 1.42 (8-bit, 20480 x 1024).  On either side of the limits, us:
+//   16-bit, 8 tokens, BF16 on E8M0: 40960 x 2048: 16 x 1 10.8, 32 x 2 14.2;  57344 x 4096: 34.1 and 29.8;  20480 x 6144 (FP16): 14.4 and 18.2;  14336 x 8192
+//     (FP16) and longer rows: 32 x 2
+//   16-bit, 14 tokens: 20480 x 4096: 16 x 1 13.1, 32 x 1 13.4, 64 x 1 17.4;  24576 x 8192: 16 x 1 a fifth slower than 32 x 1;  28672 x 4096 18.5 with 64 x 1, 16.1 with
+//     32 x 1;  131072 x 2048 55 and 45;  128256 x 8192 134 and 142, but on UE4M3 193 and 171
+//   8-bit, 14 tokens: 20000 x 5120: 32 x 2 18.4, 32 x 1 14.2;  28672 x 8192: 27 and 31;  131072 x 2048: 41 and 35
 template <int AT, int SF> static mmaemu_status launch_stream_typed(const ProductArgs &p, hipStream_t s)
 {
     constexpr bool BYTES = AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2, E8M0 = SF == MMAEMU_SCALE_FORMAT_E8M0;
@@ -233,12 +239,12 @@ template <int AT, int SF> static mmaemu_status launch_stream_typed(const Product
         }
         if (few) return launch_stream<AT, SF, 16, 1, 2, 8>(p, s);
         if (resident) return launch_stream<AT, SF, 16, 1, 2, 4>(p, s);
-        return p.n > 16384 && p.n <= 24576 ? launch_stream<AT, SF, 16, 2, 1, 4>(p, s) : launch_stream<AT, SF, 16, 2, 2, 4>(p, s);
+        return p.n > 16384 && p.k <= (p.n <= 24576 ? 6144 : 2048) ? launch_stream<AT, SF, 16, 2, 1, 4>(p, s) : launch_stream<AT, SF, 16, 2, 2, 4>(p, s);
     } else {
         if (p.m <= 8) {
             if (few) return launch_stream<AT, SF, 8, 1, 2, 8>(p, s);
             if (resident) return launch_stream<AT, SF, 8, 1, 2, 4>(p, s);
-            return p.n <= 20480 && p.k <= 6144 ? launch_stream<AT, SF, 8, 1, 1, 4>(p, s) : launch_stream<AT, SF, 8, 2, 2, 4>(p, s);
+            return p.k <= (p.n <= 20480 ? 6144 : 2048) ? launch_stream<AT, SF, 8, 1, 1, 4>(p, s) : launch_stream<AT, SF, 8, 2, 2, 4>(p, s);
         }
         if (few) return launch_stream<AT, SF, 16, 1, 1, 8>(p, s);
         if (resident && p.k <= 4096) return launch_stream<AT, SF, 16, 1, 1, 4>(p, s);
@@ -246,8 +252,10 @@ template <int AT, int SF> static mmaemu_status launch_stream_typed(const Product
             if constexpr (E8M0) return launch_stream<AT, SF, 16, 2, 2, 4>(p, s);
             else return launch_stream<AT, SF, 16, 2, 1, 8>(p, s);
         }
-        if (p.n <= 16384) return launch_stream<AT, SF, 16, 2, 1, 4>(p, s);
-        return (p.n - 1) % 16384 < 8192 ? launch_stream<AT, SF, 16, 1, 1, 4>(p, s) : launch_stream<AT, SF, 16, 4, 1, 4>(p, s);
+        if (p.n > 16384 && p.n <= 24576 && p.k <= 6144) return launch_stream<AT, SF, 16, 1, 1, 4>(p, s);
+        if constexpr (E8M0)
+            if (p.n > 24576 && p.k > 6144) return launch_stream<AT, SF, 16, 4, 1, 4>(p, s);
+        return launch_stream<AT, SF, 16, 2, 1, 4>(p, s);
     }
 }
 

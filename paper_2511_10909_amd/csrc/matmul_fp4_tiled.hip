@@ -432,6 +432,8 @@ template <int AT, int SF, int BM, int BN, int TM, int TN, int WK, int S, Order O
 //   512 tokens, 8192 x 8192: 128 x 128 36 and 63, 64 x 128 45 and 66;      8192 x 2048: 128 x 128 15 and 23, 64 x 128 17 and 21
 //   256 tokens, 8192 x 8192: 64 x 128 23 and 36, 64 x 64 26 and 43, 128 x 128 35 and 61
 //   128 tokens: 64 x 64 16 and 22, 32 x 64 21 and 26;  64 tokens: 32 x 64 12 and 16, 64 x 64 16 and 21, 32 x 32 15 and 22;  32 tokens: 32 x 32 9.5 and 12, 32 x 64 12 and 16
+// The other kinds go by the same times: on nineteen sizes of 64 to 4096 tokens FP16 on NVFP4 took at most 6 % more than in its fastest block, BF16 on
+// NVFP4 6 (256 tokens, 28672 x 8192: 190 us, 180 in the same blocks unsplit), FP16 on MXFP4 11 (1024 tokens, 4096 x 4096: 64 x 128 49, 128 x 128 44).
 struct BlockTimes { float one[2], two[2]; };       // [0]: 8-bit activations, [1]: 16-bit ones
 struct BlockChoice { uint32_t bm, bn; BlockTimes at_2048, at_8192; };
 static const BlockChoice BLOCK_CHOICES[] = {
@@ -517,8 +519,9 @@ template <int AT, int SF> static mmaemu_status launch_block(const ProductArgs &p
     constexpr bool BYTES = AT == MMAEMU_FP8_E4M3 || AT == MMAEMU_FP8_E5M2, TWO_WAYS = AT == MMAEMU_FP16 && SF == MMAEMU_SCALE_FORMAT_E8M0;
     switch (block) {
     // (the wavefront's share, the depth of the buffers and the reading ahead: what was fastest for each kind of activations; deeper buffers
-    // than three gain nothing; wavefronts that take weights to 16 bits have fewer of them and more tokens: 2048 x 8192 x 4096 under UE4M3
-    // scales 191 -> 144 us; 8-bit ones have no such work, and sixteen wavefronts in the smallest blocks: 64 E4M3 tokens on 8192 x 8192 12.7 ->
+    // than three gain nothing; wavefronts that take weights to 16 bits have fewer of them and more tokens: 2048 x 8192 x 4096 in
+    // 64 x 128 and 128 x 64 a wavefront, under UE4M3 scales BF16 172 and 137 us, FP16 124 and 113, BF16 under E8M0 110 and 106; 8-bit ones have
+    // no such work (55 and 58), and sixteen wavefronts in the smallest blocks: 64 E4M3 tokens on 8192 x 8192 12.7 ->
     // 11.8, 16-bit ones 16.2 -> 18.3; 128 BF16 tokens on 8192 x 8192 in 64 x 64: 30 us with 32 x 32 a wavefront, 22 with 64 x 32)
     case 0:
         if constexpr (BYTES) return launch_tile<AT, SF, 256, 256, 64, 128, 1, 3, Order::TURNS>(p, s);

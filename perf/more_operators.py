@@ -1,0 +1,472 @@
+"""Measured cases of the operators around a cache held in 4 bits: what fills it, what reads it, what moves its pages.
+
+Three operators that follow one another in a program that serves a language model: queries and keys normed for each head and
+rotated by their positions, keys and values brought to MXFP4 and put into the cache's pages (kind "append"); attention over those
+pages, from one token of one sequence to a whole prompt (kind "attention"); copies of pages, as a fork or a compaction of
+sequences asks for them (kind "copy").  Each case is one call of one operator on one layer's data.
+
+The cache: pages of `page` tokens (a multiple of 32), each of all KV heads, a head's tokens in granules of 32.  A granule is 34 D
+bytes for heads of D elements: K codes (16 D), V codes (16 D), K scales (D), V scales (D), in the order that `_granules` writes out.
+Elements are E2M1 under an E8M0 scale per 32 elements of a token's head, 2^-23 to 2^13, so that FP16 holds every value.
+
+`run` computes the plain form in elementary torch operations where `own` is false, and makes the library's calls where it is
+true.  What the cache holds in 4 bits is returned as the numbers that codes and scales stand for (the operator writes those too, for
+programs that evaluate a quantised model); the cache itself and copied pages are bytes.
+"""
+import math
+
+import torch
+
+own = False
+
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
+EPS = 1e-6
+THETA = 10000.0
+GRID = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def listed():
+    return [
+        # One token of one sequence on its way into the cache: latency.
+        dict(name="append_token_bf16", kind="append", type="bf16", dim=128, heads=32, kv=8, page=64, sequences=1, tokens=1, length=700, ragged=False,
+             norm=True, style="halves", rotary=128, rule="floor"),
+        # A decoding batch of sequences of different lengths, scales that never saturate, pages of one granule.
+        dict(name="append_batch_fp16", kind="append", type="fp16", dim=128, heads=64, kv=8, page=32, sequences=96, tokens=1, length=2000, ragged=True,
+             norm=True, style="halves", rotary=128, rule="fit"),
+        # A prompt of 8192 tokens: bound by memory.
+        dict(name="append_prompt_bf16", kind="append", type="bf16", dim=128, heads=32, kv=8, page=128, sequences=1, tokens=8192, length=8192, ragged=False,
+             norm=True, style="halves", rotary=128, rule="floor"),
+        # Chunks of several prompts behind what the cache holds already; small heads without norms, half of each rotated, by neighbours.
+        dict(name="append_chunks_fp16", kind="append", type="fp16", dim=64, heads=12, kv=4, page=64, sequences=5, tokens=1499, length=3001, ragged=True,
+             norm=False, style="pairs", rotary=32, rule="floor"),
+        # One token over a short cache: latency.
+        dict(name="token_short_bf16", kind="attention", type="bf16", dim=128, heads=32, kv=8, page=64, sequences=1, tokens=1, length=513, ragged=False, window=0),
+        # A decoding batch, sequences of a quarter to all of 16384 tokens: the cache is read once.
+        dict(name="batch_bf16", kind="attention", type="bf16", dim=128, heads=64, kv=8, page=64, sequences=64, tokens=1, length=16384, ragged=True, window=0),
+        # One token over a long context: few rows, the tokens have to be split.
+        dict(name="token_long_fp16", kind="attention", type="fp16", dim=128, heads=32, kv=8, page=256, sequences=1, tokens=1, length=131072, ragged=False, window=0),
+        # Drafted tokens of several sequences, verified together; small heads in groups of seven, a sliding window.
+        dict(name="drafts_window_bf16", kind="attention", type="bf16", dim=64, heads=28, kv=4, page=32, sequences=24, tokens=5, length=9001, ragged=True, window=4096),
+        # A prompt by itself: causal, bound by the matrix instructions.
+        dict(name="prompt_bf16", kind="attention", type="bf16", dim=128, heads=32, kv=8, page=128, sequences=1, tokens=8192, length=8192, ragged=False, window=0),
+        # Chunks of prompts of different lengths over what the cache holds of each.
+        dict(name="chunks_fp16", kind="attention", type="fp16", dim=128, heads=32, kv=4, page=64, sequences=6, tokens=1030, length=6007, ragged=True, window=0),
+        # The last pages of sixteen sequences that fork, one layer: latency.
+        dict(name="copy_fork", kind="copy", dim=128, kv=8, page=32, layers=1, pages=640, moves=16),
+        # A compaction of all layers' pages.
+        dict(name="copy_compact", kind="copy", dim=128, kv=8, page=64, layers=16, pages=384, moves=150),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(("append", "append", "attention", "attention", "attention", "copy"))
+    while True:
+        dim, kv, page = rng.choice((64, 128, 128)), rng.choice((1, 2, 4, 8)), rng.choice((32, 64, 128, 256))
+        c = dict(kind=kind, type=rng.choice(("bf16", "bf16", "fp16")), dim=dim, heads=kv * rng.choice((1, 2, 3, 4, 5, 7, 8, 16)), kv=kv, page=page)
+        few = rng.random() < 0.5                    # single tokens and drafts, or prompts
+        if kind == "append":
+            c.update(sequences=_log(rng, 1, 128) if few else _log(rng, 1, 8), tokens=rng.choice((1, 1, 2, 5)) if few else _log(rng, 6, 8192), ragged=rng.random() < 0.7,
+                     norm=rng.random() < 0.7, style=rng.choice(("halves", "pairs")), rotary=rng.choice((0, dim // 2, dim, dim)), rule=rng.choice(("floor", "fit")))
+            c["length"] = c["tokens"] + _log(rng, 1, 8192)
+            if c["sequences"] * c["tokens"] * (c["heads"] + 2 * kv) * dim <= 8192 * 48 * 128 and c["sequences"] * c["length"] * kv * dim <= 1 << 28:
+                return c
+        elif kind == "attention":
+            c.update(sequences=_log(rng, 1, 96) if few else _log(rng, 1, 8), tokens=rng.choice((1, 1, 2, 5)) if few else _log(rng, 6, 4096), ragged=rng.random() < 0.7)
+            c["length"] = c["tokens"] + _log(rng, 1, 65536 if few else 8192)
+            c["window"] = rng.choice((0, 0, _log(rng, 16, 8192)))
+            held, pairs = c["sequences"] * c["length"] * kv * dim, c["sequences"] * c["tokens"] * c["length"] * c["heads"] * dim
+            if held <= 64 * 16384 * 8 * 128 * 5 // 8 and pairs <= 8192 * 4096 * 32 * 128:
+                return c
+        else:
+            c = dict(kind=kind, dim=dim, kv=kv, page=page, layers=_log(rng, 1, 32), pages=_log(rng, 16, 4096))
+            c["moves"] = max(1, min(c["pages"] // 2, _log(rng, 1, 512)))
+            per_page = 34 * dim * kv * page // 32
+            if c["layers"] * c["pages"] * per_page <= 16 * 384 * 69632 and c["layers"] * c["moves"] * per_page <= 16 * 150 * 69632:
+                return c
+
+
+def _sizes(case):
+    """Tokens that come with the call and tokens in the cache after them, for each sequence: from the case alone."""
+    n, length = [], []
+    for s in range(case["sequences"]):
+        f, g = (1.0 - 0.75 * (0.6180339887 * s % 1.0), 1.0 - 0.8 * (0.7548776662 * s % 1.0)) if case["ragged"] else (1.0, 1.0)
+        n.append(max(1, int(case["tokens"] * g)))
+        length.append(max(n[-1], int(case["length"] * f)))
+    return n, length
+
+
+def _first(case, n, length, i):
+    """First token that query token i of a sequence sees."""
+    return max(0, length - n + i + 1 - case["window"]) if case["window"] else 0
+
+
+def work(case):
+    if case["kind"] == "copy":
+        return {"bytes": 2 * case["layers"] * case["moves"] * 34 * case["dim"] * case["kv"] * case["page"] // 32, "flops": 0}
+    n, length = _sizes(case)
+    d, heads, kv = case["dim"], case["heads"], case["kv"]
+    tokens = sum(n)
+    if case["kind"] == "append":
+        # the cache's part in 17/32 bytes an element, and the values that it stands for
+        return {"bytes": tokens * ((heads + 2 * kv) * d * 2 + heads * d * 2 + 2 * kv * d * 17 // 32 + 2 * kv * d * 2 + 4 * case["rotary"]), "flops": tokens * (heads + kv) * d * 8}
+    seen = sum(l - _first(case, a, l, 0) for a, l in zip(n, length))
+    pairs = sum(sum(l - a + i + 1 - _first(case, a, l, i) for i in range(a)) for a, l in zip(n, length))
+    return {"bytes": seen * 2 * kv * d * 17 // 32 + 4 * tokens * heads * d, "flops": 4 * pairs * heads * d}
+
+
+# ---- inputs -------------------------------------------------------------------------------
+
+def _heads(shape, gen, std=1.0):
+    """Heads of different sizes, a few of whose elements are far larger than the rest in every token."""
+    x = torch.randn(shape, generator=gen, device="cuda")
+    x *= std * torch.exp(0.3 * torch.randn(shape[:-1] + (1,), generator=gen, device="cuda"))
+    x[..., ::29] *= 4.0
+    return x
+
+
+def _tables(case, gen):
+    """Page tables with the pages in no order, lengths, and where each sequence's tokens begin."""
+    n, length = _sizes(case)
+    page = case["page"]
+    wide = max(-(-l // page) for l in length)
+    counts = [-(-l // page) for l in length]
+    order = torch.randperm(sum(counts) + 2, generator=gen, device="cuda").to(torch.int32)
+    table = torch.full((case["sequences"], wide), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for s, c in enumerate(counts):
+        table[s, :c] = order[at:at + c]
+        at += c
+    begins = torch.tensor([0] + n, dtype=torch.int32).cumsum(0).to(torch.int32).cuda()
+    return dict(table=table, lengths=torch.tensor(length, dtype=torch.int32).cuda(), begins=begins, pages=sum(counts) + 2, tokens=sum(n), most=max(n), longest=max(length))
+
+
+def _granules(k, v, ks, vs):
+    """Codes [page][tokens][kv][D / 2] (two to a byte) and scale codes [page][tokens][kv][D / 32] as the cache's pages: [page][kv][granule][34 D]."""
+    p, t, kv, half = k.shape
+    g, b = t // 32, ks.shape[-1]
+    if half == 64:
+        # K: token 8 w + 4 a + r of the granule, 32 elements o of it: 16 bytes at [a][o][w][r];  V: tokens 8 o + t, elements 8 d + 4 c + 2 p and the
+        # next as one byte at [c][o][d][p][t]
+        kc = k.reshape(p, g, 4, 2, 4, kv, 4, 16).permute(0, 5, 1, 3, 6, 2, 4, 7)
+        vc = v.reshape(p, g, 4, 8, kv, 16, 2, 2).permute(0, 4, 1, 6, 2, 5, 7, 3)
+    else:
+        # K: 16 elements o, 8 bytes at [o][w][r][a];  V: elements 4 d + 2 p and the next at [o][d][p][t]
+        kc = k.reshape(p, g, 4, 2, 4, kv, 4, 8).permute(0, 5, 1, 6, 2, 4, 3, 7)
+        vc = v.reshape(p, g, 4, 8, kv, 16, 2).permute(0, 4, 1, 2, 5, 6, 3)
+    # scales: K as [block][w, r][a], V as [o][block][t]
+    sk = ks.reshape(p, g, 4, 2, 4, kv, b).permute(0, 5, 1, 6, 2, 4, 3)
+    sv = vs.reshape(p, g, 4, 8, kv, b).permute(0, 4, 1, 2, 5, 3)
+    return torch.cat([x.reshape(p, kv, g, -1) for x in (kc, vc, sk, sv)], dim=-1)
+
+
+def _filled(case, pages, gen):
+    """A cache whose pages are all full: keys as a norm leaves them, values of a few tenths."""
+    page, kv, d = case["page"], case["kv"], case["dim"]
+    memory = torch.empty((pages, kv, page // 32, 34 * d), dtype=torch.uint8, device="cuda")
+    step = max(1, (1 << 26) // (page * kv * d))
+    for p in range(0, pages, step):
+        shape = (min(step, pages - p), page, kv, d)
+        parts = []
+        for std in (1.0, 0.3):
+            code, scale, _ = _quantize_plain(_heads(shape, gen, std), "floor")
+            parts.append((code[..., 0::2] | (code[..., 1::2] << 4), scale))
+        memory[p:p + shape[0]] = _granules(parts[0][0], parts[1][0], parts[0][1], parts[1][1])
+    return memory
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    d, kv, page = case["dim"], case["kv"], case["page"]
+    s = dict(case=case)
+    if case["kind"] == "copy":
+        per_page = 34 * d * kv * page // 32
+        s["memory"] = torch.randint(0, 256, (case["layers"], case["pages"], per_page), generator=gen, dtype=torch.uint8, device="cuda")
+        order = torch.randperm(case["pages"], generator=gen, device="cuda")[:2 * case["moves"]].to(torch.int32).cpu()
+        s["moves"] = order.reshape(-1, 2).contiguous()                # (from, to): what a program's page tables keep on the host
+        return s
+    t, heads = TYPES[case["type"]], case["heads"]
+    s.update(_tables(case, gen))
+    tokens = s["tokens"]
+    if case["kind"] == "append":
+        # the three projections' output, one row a token
+        s["qkv"] = _heads((tokens, heads + 2 * kv, d), gen).to(t).reshape(tokens, -1)
+        s["q"], s["k"], s["v"] = s["qkv"].split((heads * d, kv * d, kv * d), dim=1)
+        s["qw"], s["kw"] = ((1 + 0.2 * torch.randn(d, generator=gen, device="cuda")).to(t) for _ in range(2)) if case["norm"] else (None, None)
+        s["rotation"] = None
+        if case["rotary"]:
+            # 64 bits: the angles of far positions
+            angle = torch.arange(s["longest"], device="cuda", dtype=torch.float64)[:, None] * THETA ** (-torch.arange(0, case["rotary"], 2, device="cuda", dtype=torch.float64) / case["rotary"])
+            s["rotation"] = torch.cat((angle.cos(), angle.sin()), dim=1).float()
+        s["cache"] = torch.zeros((s["pages"], kv, page // 32, 34 * d), dtype=torch.uint8, device="cuda")
+        s["q_out"] = torch.empty((tokens, heads * d), dtype=t, device="cuda")
+        s["k_values"], s["v_values"] = (torch.empty((tokens, kv * d), dtype=t, device="cuda") for _ in range(2))
+        return s
+    s["q"] = (1.5 * _heads((tokens, heads, d), gen)).to(t).reshape(tokens, -1)
+    s["cache"] = _filled(case, s["pages"], gen)
+    s["out"] = torch.empty((tokens, heads * d), dtype=t, device="cuda")
+    s["workspace"] = None
+    return s
+
+
+# ---- the operators, plain -----------------------------------------------------------------
+
+def _quantize_plain(x, rule):
+    """x (binary32, [..., D]): E2M1 codes, one a byte, E8M0 codes, and the values that both stand for, in binary32."""
+    v = x.reshape(x.shape[:-1] + (x.shape[-1] // 32, 32))
+    amax = v.abs().amax(-1, keepdim=True)
+    mant, e = torch.frexp(amax)
+    e = e - 3
+    if rule == "fit":
+        e = e + (mant > 0.75).to(e.dtype)
+    e = torch.where(amax == 0, -23, e).clamp(-23, 13)
+    q = torch.ldexp(v, -e)
+    a = q.abs()
+    code = ((a > 0.25).to(torch.uint8) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0)).to(torch.uint8)
+    value = torch.tensor(GRID, device=x.device)[code.int()]
+    value = torch.ldexp(torch.where(torch.signbit(q), -value, value), e).reshape(x.shape)
+    code = code | (torch.signbit(q).to(torch.uint8) << 3)
+    return code.reshape(x.shape), (e + 127).to(torch.uint8).squeeze(-1), value
+
+
+def _positions(s):
+    """For each token of the call: its sequence, and its position there."""
+    at = torch.arange(s["tokens"], device="cuda", dtype=torch.int32)
+    of = torch.searchsorted(s["begins"][1:], at, right=True)
+    n = s["begins"][1:] - s["begins"][:-1]
+    return of, s["lengths"][of] - n[of] + at - s["begins"][of]
+
+
+def _rotated(y, s, positions):
+    case = s["case"]
+    r = case["rotary"]
+    if not r:
+        return y
+    angles = s["rotation"][positions].double()
+    cos, sin = angles[:, None, :r // 2], angles[:, None, r // 2:]
+    if case["style"] == "halves":
+        a, b = y[..., :r // 2], y[..., r // 2:r]
+        turned = torch.cat((a * cos - b * sin, b * cos + a * sin), dim=-1)
+    else:
+        a, b = y[..., 0:r:2], y[..., 1:r:2]
+        turned = torch.stack((a * cos - b * sin, b * cos + a * sin), dim=-1).flatten(-2)
+    return torch.cat((turned, y[..., r:]), dim=-1)
+
+
+def _append_plain(s):
+    case = s["case"]
+    d, tokens, t = case["dim"], s["tokens"], TYPES[case["type"]]
+    of, positions = _positions(s)
+
+    def normed(x, w):
+        # 64 bits: a value next to a border between two codes must not cross it
+        y = x.reshape(tokens, -1, d).double()
+        if w is not None:
+            y = y * (1.0 / torch.sqrt((y * y).mean(-1, keepdim=True) + EPS)) * w.double()
+        return _rotated(y, s, positions).float()
+
+    q = normed(s["q"], s["qw"]).to(t).reshape(tokens, -1)
+    kc, ks, k = _quantize_plain(normed(s["k"], s["kw"]), case["rule"])
+    vc, vs, v = _quantize_plain(s["v"].reshape(tokens, -1, d).float(), case["rule"])
+    # where the granule has each byte: of the two elements 2 e and 2 e + 1, and of block e
+    page, kv = case["page"], case["kv"]
+    slot = positions % page
+    granule = (s["table"][of, positions // page].long() * kv * (page // 32) + slot // 32)[:, None] + torch.arange(kv, device="cuda") * (page // 32)
+    x = (slot % 32)[:, None, None]
+    w, a, r, b = x // 8, x // 4 % 2, x % 4, x % 8
+    e = torch.arange(0, d, 2, device="cuda")
+    if d == 128:
+        at_k = a * 1024 + e // 32 * 256 + (4 * w + r) * 16 + e % 32 // 2
+        at_v = e // 4 % 2 * 1024 + w * 256 + e // 8 * 16 + e // 2 % 2 * 8 + b
+    else:
+        at_k = e // 16 * 256 + (4 * w + r) * 16 + a * 8 + e % 16 // 2
+        at_v = w * 256 + e // 4 * 16 + e // 2 % 2 * 8 + b
+    e = torch.arange(d // 32, device="cuda")
+    to = s["cache"].reshape(-1)
+    begin = granule[..., None] * (34 * d)
+    to[begin + at_k] = kc[..., 0::2] | (kc[..., 1::2] << 4)
+    to[begin + 16 * d + at_v] = vc[..., 0::2] | (vc[..., 1::2] << 4)
+    to[begin + 32 * d + (e * 16 + 4 * w + r) * 2 + a] = ks
+    to[begin + 33 * d + (w * (d // 32) + e) * 8 + b] = vs
+    return dict(q=q, k=k.to(t).reshape(tokens, -1), v=v.to(t).reshape(tokens, -1), cache=s["cache"])
+
+
+def _read_plain(s):
+    """The cache's keys and values of all sequences, [sequences][kv][tokens of the longest table][D], binary32."""
+    case = s["case"]
+    d, kv, page, n = case["dim"], case["kv"], case["page"], case["sequences"]
+    x = s["cache"][s["table"].clamp(min=0).reshape(-1)]
+    g, b = page // 32, d // 32
+    kc, vc, sk, sv = x.split((16 * d, 16 * d, d, d), dim=-1)
+    lead = (n, -1, kv, g)                            # sequences, pages, heads, granules
+    if d == 128:
+        kc = kc.reshape(lead + (2, 4, 4, 4, 16)).permute(0, 2, 1, 3, 6, 4, 7, 5, 8)
+        vc = vc.reshape(lead + (2, 4, 16, 2, 8)).permute(0, 2, 1, 3, 5, 8, 6, 4, 7)
+    else:
+        kc = kc.reshape(lead + (4, 4, 4, 2, 8)).permute(0, 2, 1, 3, 5, 7, 6, 4, 8)
+        vc = vc.reshape(lead + (4, 16, 2, 8)).permute(0, 2, 1, 3, 4, 7, 5, 6)
+    sk = sk.reshape(lead + (b, 4, 4, 2)).permute(0, 2, 1, 3, 5, 7, 6, 4)
+    sv = sv.reshape(lead + (4, b, 8)).permute(0, 2, 1, 3, 4, 6, 5)
+    lut = torch.tensor(GRID, device="cuda")
+    lut = torch.cat((lut, -lut))
+
+    def values(c, scale):
+        c, scale = c.reshape(n, kv, -1, d // 2), scale.reshape(n, kv, -1, b)
+        y = lut[torch.stack((c & 15, c >> 4), dim=-1).reshape(n, kv, -1, b, 32).int()]
+        return (y * torch.exp2(scale.float() - 127).unsqueeze(-1)).reshape(n, kv, -1, d)
+
+    return values(kc, sk), values(vc, sv)
+
+
+def _attention_plain(s):
+    case = s["case"]
+    d, heads, kv, n, most, t = case["dim"], case["heads"], case["kv"], case["sequences"], s["most"], TYPES[case["type"]]
+    group = heads // kv
+    k, v = _read_plain(s)
+    of, positions = _positions(s)
+    slot = torch.arange(s["tokens"], device="cuda") - s["begins"][of]
+    # queries in a padded batch: [sequence][kv][token, head of the group][D]
+    q = torch.zeros((n, most, kv, group, d), device="cuda")
+    q[of, slot] = s["q"].float().reshape(-1, kv, group, d)
+    q = q.permute(0, 2, 1, 3, 4).reshape(n * kv, most * group, d)
+    at = torch.full((n, most), -1, dtype=torch.int32, device="cuda")
+    at[of, slot] = positions
+    token = torch.arange(k.shape[2], device="cuda", dtype=torch.int32)
+    seen = token <= at[..., None]
+    if case["window"]:
+        seen &= token > at[..., None] - case["window"]
+    scores = torch.matmul(q, k.reshape(n * kv, -1, d).transpose(1, 2).contiguous()) * (1.0 / math.sqrt(d))
+    scores = scores.reshape(n, kv, most, group, -1).masked_fill_(~seen[:, None, :, None, :], -math.inf)
+    scores -= scores.amax(-1, keepdim=True)
+    p = scores.exp_()
+    p /= p.sum(-1, keepdim=True)
+    o = torch.matmul(p.reshape(n * kv, most * group, -1), v.reshape(n * kv, -1, d))
+    return o.reshape(n, kv, most, group, d).permute(0, 2, 1, 3, 4)[of, slot].reshape(-1, heads * d).to(t)
+
+
+def _copy_plain(s):
+    moves = s["moves"].cuda().long()
+    s["memory"][:, moves[:, 1]] = s["memory"][:, moves[:, 0]]
+    return s["memory"]
+
+
+def run(s):
+    case = s["case"]
+    kind = case["kind"]
+    if not own:
+        return {"append": _append_plain, "attention": _attention_plain, "copy": _copy_plain}[kind](s)
+    from paper_2511_10909_amd import binding as mm
+    if kind == "copy":
+        mm.cache_copy_pages(s["memory"], s["moves"], case["pages"], s["memory"].shape[2], case["layers"])
+        return s["memory"]
+    t = {"bf16": mm.BF16, "fp16": mm.FP16}[case["type"]]
+    shape = dict(dim=case["dim"], heads=case["heads"], kv_heads=case["kv"], page_tokens=case["page"], pages=s["pages"], sequences=case["sequences"],
+                 table_stride=s["table"].shape[1], tokens=s["tokens"], max_tokens=s["most"])
+    if kind == "append":
+        stride = s["qkv"].shape[1]
+        mm.cache_append_fp4(s["q"], s["k"], s["v"], s["q_out"], s["cache"], s["table"], s["lengths"], s["begins"], t, **shape, q_weight=s["qw"], k_weight=s["kw"],
+                            rotation=s["rotation"], rotary_dim=case["rotary"], rotation_rows=s["longest"],
+                            rotation_style=mm.ROTATE_HALVES if case["style"] == "halves" else mm.ROTATE_PAIRS,
+                            scale_rule=mm.SCALE_RULE_FIT if case["rule"] == "fit" else mm.SCALE_RULE_FLOOR, eps=EPS,
+                            q_stride=stride, k_stride=stride, v_stride=stride, k_values=s["k_values"], v_values=s["v_values"])
+        return dict(q=s["q_out"], k=s["k_values"], v=s["v_values"], cache=s["cache"])
+    if s["workspace"] is None:                       # as a program keeps it for all its calls
+        size = mm.attention_fp4_workspace(t, max_length=s["longest"], **shape)
+        s["workspace"] = torch.empty(max(size, 16), dtype=torch.uint8, device="cuda")
+    mm.attention_fp4(s["q"], s["out"], s["cache"], s["table"], s["lengths"], s["begins"], s["workspace"], t, max_length=s["longest"],
+                     window=case["window"], scale=1.0 / math.sqrt(case["dim"]), workspace_bytes=s["workspace"].numel(), **shape)
+    return s["out"]
+
+
+# ---- the same from the definitions, in 64 bits ----------------------------------------------
+
+def _nearest(v, mant, emin, top):
+    """v rounded to the nearest multiple of its unit in the last place (ties to even), saturated: `mant` mantissa bits, least exponent `emin`."""
+    _, e = torch.frexp(v)
+    unit = torch.ldexp(torch.ones_like(v), torch.clamp(e - 1, min=emin) - mant)
+    return torch.clamp(torch.round(v / unit) * unit, -top, top)
+
+
+def _exact_fp4(y, rule):
+    b = y.unflatten(-1, (-1, 32))
+    amax = b.abs().max(dim=-1, keepdim=True).values
+    p = torch.exp2(torch.floor(torch.log2(amax)) - 2)
+    if rule == "fit":
+        p = torch.where(amax > 6 * p, 2 * p, p)
+    p = p.clamp(2.0 ** -23, 2.0 ** 13)
+    return (_nearest(b / p, 1, 0, 6.0) * p).flatten(-2)
+
+
+def _exact_append(s):
+    case = s["case"]
+    d, heads, kv, r = case["dim"], case["heads"], case["kv"], case["rotary"]
+    n, length = _sizes(case)
+    x = s["qkv"].double().reshape(s["tokens"], heads + 2 * kv, d)
+    y = x[:, :heads + kv].clone()
+    if case["norm"]:
+        w = torch.cat((s["qw"].double().expand(heads, d), s["kw"].double().expand(kv, d)))
+        y = y * w / torch.sqrt(y.square().sum(-1, keepdim=True) / d + EPS)
+    if r:
+        at = torch.cat([torch.arange(l - a, l) for a, l in zip(n, length)]).cuda()
+        # the table's own numbers: complex factors, element i of the first part with its partner
+        table = s["rotation"].double()[at]
+        turn = torch.complex(table[:, :r // 2], table[:, r // 2:])[:, None]
+        i = torch.arange(r // 2, device="cuda")
+        re, im = (i, i + r // 2) if case["style"] == "halves" else (2 * i, 2 * i + 1)
+        z = torch.complex(y[..., re], y[..., im]) * turn
+        y[..., re], y[..., im] = z.real, z.imag
+    k, v = _exact_fp4(y[:, heads:], case["rule"]), _exact_fp4(x[:, heads + kv:], case["rule"])
+    return dict(q=y[:, :heads].flatten(1), k=k.flatten(1), v=v.flatten(1), cache=None)
+
+
+def _exact_bytes(case, memory, pages):
+    """Keys and values of one sequence's pages, [tokens][kv][D] in binary64, element by element from the granule's description."""
+    d, kv, page = case["dim"], case["kv"], case["page"]
+    x = memory[pages].permute(0, 2, 1, 3).reshape(-1, kv, 34 * d)       # granules of the sequence in order
+    t, e = torch.arange(32, device="cuda")[:, None], torch.arange(d, device="cuda")[None, :]
+    w, a, r, o = t // 8, t // 4 % 2, t % 4, t // 8
+    if d == 128:
+        at_k = a * 1024 + e // 32 * 256 + (4 * w + r) * 16 + e % 32 // 2
+        at_v = 2048 + e // 4 % 2 * 1024 + o * 256 + e // 8 * 16 + e // 2 % 2 * 8 + t % 8
+    else:
+        at_k = e // 16 * 256 + (4 * w + r) * 16 + a * 8 + e % 16 // 2
+        at_v = 1024 + o * 256 + e // 4 * 16 + e // 2 % 2 * 8 + t % 8
+    at_sk = 32 * d + (e // 32 * 16 + 4 * w + r) * 2 + a
+    at_sv = 33 * d + (o * (d // 32) + e // 32) * 8 + t % 8
+    out = []
+    for at, at_scale in ((at_k, at_sk), (at_v, at_sv)):
+        c = (x[..., at.flatten()].int() >> (4 * (e % 2)).expand(32, d).flatten()) & 15
+        m, f = c & 1, (c >> 1) & 3
+        value = torch.where(f > 0, (2 + m) * torch.exp2(f.double() - 2), m * 0.5)
+        value = torch.where(c > 7, -value, value) * torch.exp2(x[..., at_scale.flatten()].double() - 127)
+        out.append(value.reshape(-1, kv, 32, d).permute(0, 2, 1, 3).reshape(-1, kv, d))
+    return out
+
+
+def _exact_attention(s):
+    case = s["case"]
+    d, heads, kv = case["dim"], case["heads"], case["kv"]
+    group = heads // kv
+    n, length = _sizes(case)
+    out = torch.empty((s["tokens"], heads, d), dtype=torch.float64, device="cuda")
+    row = 0
+    for i, (a, l) in enumerate(zip(n, length)):
+        k, v = _exact_bytes(case, s["cache"], s["table"][i, :-(-l // case["page"])].long())
+        q = s["q"][row:row + a].double().reshape(a, heads, d)
+        pos, tok = torch.arange(l - a, l, device="cuda"), torch.arange(l, device="cuda")
+        hidden = tok[None, :] > pos[:, None]
+        if case["window"]:
+            hidden |= tok[None, :] <= pos[:, None] - case["window"]
+        for h in range(heads):
+            z = torch.mm(q[:, h], k[:l, h // group].t()) / math.sqrt(d)
+            out[row:row + a, h] = torch.mm(torch.softmax(z.masked_fill(hidden, -math.inf), dim=1), v[:l, h // group])
+        row += a
+    return out.reshape(s["tokens"], -1)
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return None if case["kind"] == "copy" else {"append": _exact_append, "attention": _exact_attention}[case["kind"]](s)

@@ -632,6 +632,95 @@ mmaemu_status mmaemu_matmul_fp4_packed(const mmaemu_matmul_fp4_args *args);
 mmaemu_status mmaemu_matmul_fp4_kernel(uint32_t m, uint32_t n, uint32_t k, mmaemu_dtype a_type, uint32_t scale_format, const char **name);
 
 /*
+ * A cache of keys and values in 4 bits (MXFP4: E2M1 elements, an E8M0 scale per 32 elements of a token's head), what fills it, what reads it
+ * and what moves its pages.  memory: pages of page_tokens tokens (a multiple of 32), each of all kv_heads heads of `dim` elements (64 or 128):
+ * page_tokens * kv_heads * dim * 17 / 16 bytes a page; the bytes of a granule of 32 tokens of a head are described in cache_fp4.hpp.  Scale
+ * codes are 104 .. 140, so that FP16 holds every value: a block whose rule asks for a larger scale saturates at 6 * 2^13, one that asks for a smaller
+ * takes 2^-23.  A block that holds an infinity or a NaN takes code 255 and reads as NaN.  Other codes are not for the cache: what a reader
+ * makes of them is not specified.
+ *
+ * A call works on `sequences` sequences.  DEVICE arrays of 32-bit integers, read when the work runs:
+ *   table[sequences][table_stride]  pages of each sequence in order; token t lies in page table[s][t / page_tokens]
+ *   lengths[sequences]              tokens of each sequence in the cache, those that come with the call included; clipped to 0 .. table_stride *
+ *                                   page_tokens
+ *   begins[sequences + 1]           rows of sequence s among the call's `tokens` rows: begins[s] .. begins[s + 1] - 1; clipped to 0 .. tokens, none
+ *                                   where begins[s + 1] < begins[s]
+ * Row i of the n rows of a sequence is its token of position lengths[s] - n + i.  max_tokens is the host's bound for n: rows from max_tokens on
+ * are neither computed nor written.  Rows that belong to no sequence are left as they are.  No table entry is followed unless it lies in
+ * 0 .. pages - 1: tokens of other pages are not written, and read as if they were not there.
+ *
+ * type BF16 or FP16.  Row t of an array starts at element t * its stride (0: its row's length); strides and pointers of q, k, v, out, q_out multiples of
+ * 8 elements (16 bytes).  sequences = 0, tokens = 0 or max_tokens = 0 is a no-op.  All calls work while captured into a graph.
+ */
+enum { MMAEMU_ROTATE_HALVES = 0, MMAEMU_ROTATE_PAIRS = 1 };
+
+/*
+ * Queries and keys normed for each head, rotated by their positions; keys and values into the cache.
+ *   y = x / sqrt(mean(x^2) + eps) * weight for each head of q and k (weights of dim elements and of weight_type, `type` or FP32; NULL: no norm, y = x)
+ *   z: of the first rotary_dim elements of y (a multiple of 16, up to dim; 0: none), pairs (i, i + rotary_dim / 2) for HALVES, (2 i, 2 i + 1) for PAIRS,
+ *     (a, b) to (a c_i - b s_i, b c_i + a s_i), with c_i = rotation[position][i] and s_i = rotation[position][rotary_dim / 2 + i] (binary32, device memory,
+ *     rotation_rows rows; positions without a row give NaN)
+ *   binary64 throughout, rounded once to binary32; q_out: rounded to `type`; keys, and values as they came: to the cache by the scale rule
+ *   k_values, v_values: NULL, or [tokens][kv_heads * dim] of `type`: the numbers that the cache's codes stand for
+ * q_out may be q where both strides are equal; no other arrays may overlap.  No two of the call's tokens may lie in one place of the cache.
+ * q and q_out may both be NULL (heads is then 0), as may k and v (kv_heads as the cache has them; then nothing is written to the cache).
+ * Errors: SHAPE (page_tokens no multiple of 32 or above 65536, kv_heads 0 or above 1024, heads above 4096, pages 0 or above 2^30, rotary_dim, tokens above 2^30,
+ *         max_tokens above 2^24, sequences above 65535, table_stride 0 or its tokens 2^31 and more, strides below their row or above 2^32, max_tokens *
+ *         (heads + 2 kv_heads) above 2^28), INVALID_ARG (NULL or misaligned pointers, scale rule, rotation style, eps negative or not finite, q_out = q under
+ *         another stride, q without q_out, k without v, k_values or v_values without k), UNSUPPORTED (type, weight_type, dim).
+ */
+typedef struct {
+    uint32_t struct_size, type, weight_type, dim, heads, kv_heads, page_tokens, sequences, max_tokens, rotary_dim, rotation_style, scale_rule;
+    const void *q, *k, *v, *q_weight, *k_weight;
+    const float *rotation;
+    void *q_out, *k_values, *v_values, *cache;
+    const int32_t *table, *lengths, *begins;
+    uint64_t tokens, pages, table_stride, rotation_rows, q_stride, k_stride, v_stride, q_out_stride;
+    double eps;
+    void *hip_stream;
+} mmaemu_cache_append_fp4_args;
+mmaemu_status mmaemu_cache_append_fp4(const mmaemu_cache_append_fp4_args *args);
+
+/*
+ * Attention over the cache, from single tokens to prompts:
+ *   out[r][h] = sum over t of p_t v_t,  p = softmax over t of scale * (q[r][h] . k_t),  k and v of head h / (heads / kv_heads),
+ * over the tokens t <= position of row r, and > position - window where window is not 0.  A row that sees no token gives zeros.  Tokens that a row does not
+ * see have no part in it, whatever they hold.
+ * Scores, maxima and sums are binary32; the weights p, relative to a maximum, are rounded to FP16 (nearest even) for the second product.
+ * max_length: the host's bound for lengths; it decides, with the other sizes, over how many workgroups a row's tokens are split, and nothing
+ * else (longer sequences are computed all the same).  workspace: device memory of mmaemu_attention_fp4_workspace bytes, 16-byte aligned, for one call at a
+ * time: calls that share it have to follow one another, those in graphs too.  NULL where that is 0.  One launch, or two where rows are split.  Results do
+ * not depend on anything but the call's arguments and data.  out may be q where strides are equal; no other arrays may overlap.  Forward only.
+ * Errors: as above; SHAPE (heads no multiple of kv_heads, max_tokens * heads / kv_heads above 2^24), INVALID_ARG (scale not positive and finite, workspace missing,
+ *         misaligned or too small).
+ */
+typedef struct {
+    uint32_t struct_size, type, dim, heads, kv_heads, page_tokens, sequences, max_tokens, max_length, window;
+    const void *q;
+    void *out;
+    const void *cache;
+    const int32_t *table, *lengths, *begins;
+    void *workspace;
+    uint64_t tokens, pages, table_stride, q_stride, out_stride, workspace_bytes;
+    double scale;
+    void *hip_stream;
+} mmaemu_attention_fp4_args;
+mmaemu_status mmaemu_attention_fp4(const mmaemu_attention_fp4_args *args);
+/* Bytes of workspace for these arguments (pointers, strides and scale are not looked at); decided on the host, no GPU needed. */
+mmaemu_status mmaemu_attention_fp4_workspace(const mmaemu_attention_fp4_args *args, uint64_t *bytes);
+
+/*
+ * Copies pages within each of `layers` caches that lie layer_bytes apart (0: pages * page_bytes) from `memory` on: for each of `count` moves (HOST array of
+ * pairs: from, to) page `to` becomes page `from`.  All moves happen at once: no page may be the target of two moves, or the target of one and the source
+ * of another; one page may be the source of several (a fork).  A page moved onto itself is left alone.  The moves are taken when the call is made, also
+ * into a captured graph.  page_bytes: a multiple of 16 (any cache's pages are).  count = 0 or layers = 0 is a no-op.
+ * Errors: SHAPE (pages 0 or above 2^30, page_bytes 0, no multiple of 16 or above 2^32, layer_bytes below a layer's pages or no multiple of 16, layers above 65535,
+ *         a layer above 2^46 bytes), INVALID_ARG (NULL or misaligned pointers, a page outside 0 .. pages - 1, targets as above), NOMEM (host memory for the checks).
+ */
+mmaemu_status mmaemu_cache_copy_pages(void *memory, const int32_t *moves, uint64_t count, uint64_t pages, uint64_t page_bytes,
+                                      uint64_t layers, uint64_t layer_bytes, void *hip_stream);
+
+/*
  * Issue-rate probes: the measured counterpart of the vector-ALU peak that the emulation kernels' roofline is quoted
  * against (the path is bound by integer / binary32 vector-ALU issue, not by the matrix cores or HBM).  Probe `op`
  * (0 .. mmaemu_issue_probe_count() - 1, one per instruction the hot loops are made of; mmaemu_issue_probe_name gives

@@ -22,6 +22,7 @@ SCALE_FORMAT_E8M0, SCALE_FORMAT_UE4M3 = 0, 1
 GEN_ZERO, GEN_FINITE_BITS, GEN_UNIFORM_EXP, GEN_RANDOM_BITS, GEN_NORMAL = 0, 1, 2, 3, 4
 GEN_UNIFORM, GEN_NORMAL_OUTLIERS, GEN_CANCELLING, GEN_SIGNED_ZEROS = 5, 6, 7, 8
 SCALE_RULE_FLOOR, SCALE_RULE_FIT = 0, 1
+ROTATE_HALVES, ROTATE_PAIRS = 0, 1
 SCALE_NONE, SCALE_TENSOR, SCALE_TILE, SCALE_FACTOR = 0, 1, 2, 3
 (MFMA_F32_16X16X16_F16, MFMA_F32_16X16X16_BF16, MFMA_F32_32X32X8_F16, MFMA_F32_32X32X8_BF16,
  MFMA_F32_16X16X32_F16, MFMA_F32_16X16X32_BF16, MFMA_F32_16X16X32_FP8_FP8, MFMA_F32_16X16X32_FP8_BF8,
@@ -146,6 +147,10 @@ _lib.mmaemu_deviation_sample_kernel.argtypes = [_vp, _vp, _vp, _vp, _u32, _u32, 
 _lib.mmaemu_rmsnorm_quantize_packed.argtypes = [ctypes.c_char_p]
 _lib.mmaemu_quantize_fp4_packed.argtypes = [ctypes.c_char_p]
 _lib.mmaemu_matmul_fp4_packed.argtypes = [ctypes.c_char_p]
+_lib.mmaemu_cache_append_fp4.argtypes = [ctypes.c_char_p]
+_lib.mmaemu_attention_fp4.argtypes = [ctypes.c_char_p]
+_lib.mmaemu_attention_fp4_workspace.argtypes = [ctypes.c_char_p, ctypes.POINTER(_u64)]
+_lib.mmaemu_cache_copy_pages.argtypes = [_vp, _vp, _u64, _u64, _u64, _u64, _u64, _vp]
 _lib.mmaemu_matmul_fp4_kernel.argtypes = [_u32, _u32, _u32, ctypes.c_int, _u32, ctypes.POINTER(ctypes.c_char_p)]
 
 
@@ -360,6 +365,52 @@ def matmul_fp4_kernel(m, n, k, a_type, scale_format=SCALE_FORMAT_E8M0):
     name = ctypes.c_char_p()
     _check(_lib.mmaemu_matmul_fp4_kernel(m, n, k, a_type, scale_format, ctypes.byref(name)))
     return name.value.decode()
+
+
+# ---- the cache in 4 bits ------------------------------------------------------------------
+_APPEND_ARGS, _ATTENTION_ARGS = struct.Struct("@12I21QdQ"), struct.Struct("@10I13QdQ")
+_append_call, _attention_call = _lib.mmaemu_cache_append_fp4, _lib.mmaemu_attention_fp4
+
+
+def cache_page_bytes(dim, kv_heads, page_tokens):
+    """Bytes of a page of page_tokens tokens of kv_heads heads of dim elements: codes, and a scale per 32 elements, of keys and values."""
+    return page_tokens * kv_heads * dim * 17 // 16
+
+
+def cache_append_fp4(q, k, v, q_out, cache, table, lengths, begins, type, *, dim, heads, kv_heads, page_tokens, pages, sequences, table_stride, tokens, max_tokens,
+                     q_weight=None, k_weight=None, weight_type=None, rotation=None, rotary_dim=0, rotation_rows=0, rotation_style=ROTATE_HALVES,
+                     scale_rule=SCALE_RULE_FLOOR, eps=1e-6, q_stride=0, k_stride=0, v_stride=0, q_out_stride=0, k_values=None, v_values=None, stream=None):
+    """Norms and rotations of the heads of q (to q_out) and k, and k and v into the cache's pages, as table, lengths and begins (int32, on the device) have them."""
+    _check(_append_call(_APPEND_ARGS.pack(
+        _APPEND_ARGS.size, type, type if weight_type is None else weight_type, dim, heads, kv_heads, page_tokens, sequences, max_tokens, rotary_dim,
+        rotation_style, scale_rule, _address(q), _address(k), _address(v), _address(q_weight), _address(k_weight), _address(rotation), _address(q_out),
+        _address(k_values), _address(v_values), _address(cache), _address(table), _address(lengths), _address(begins), tokens, pages, table_stride,
+        rotation_rows, q_stride, k_stride, v_stride, q_out_stride, eps, _stream(stream) or 0)))
+
+
+def attention_fp4_workspace(type, *, dim, heads, kv_heads, page_tokens, pages, sequences, table_stride, tokens, max_tokens, max_length, window=0):
+    """Bytes of workspace that attention_fp4 takes for these sizes."""
+    size = _u64()
+    _check(_lib.mmaemu_attention_fp4_workspace(_ATTENTION_ARGS.pack(
+        _ATTENTION_ARGS.size, type, dim, heads, kv_heads, page_tokens, sequences, max_tokens, max_length, window, 0, 0, 0, 0, 0, 0, 0, tokens, pages, table_stride,
+        0, 0, 0, 1.0, 0), ctypes.byref(size)))
+    return size.value
+
+
+def attention_fp4(q, out, cache, table, lengths, begins, workspace, type, *, dim, heads, kv_heads, page_tokens, pages, sequences, table_stride, tokens, max_tokens,
+                  max_length, scale, window=0, q_stride=0, out_stride=0, workspace_bytes=0, stream=None):
+    """Softmax attention of the rows of q over the tokens that they see in the cache's pages; causal, window: how many tokens back a row sees (0: all)."""
+    _check(_attention_call(_ATTENTION_ARGS.pack(
+        _ATTENTION_ARGS.size, type, dim, heads, kv_heads, page_tokens, sequences, max_tokens, max_length, window, _address(q), _address(out), _address(cache),
+        _address(table), _address(lengths), _address(begins), _address(workspace), tokens, pages, table_stride, q_stride, out_stride, workspace_bytes, scale,
+        _stream(stream) or 0)))
+
+
+def cache_copy_pages(memory, moves, pages, page_bytes, layers=1, layer_bytes=0, stream=None):
+    """Copies pages within each of `layers` caches; moves: pairs (from, to), a contiguous int32 tensor on the host."""
+    if moves.dtype != torch.int32 or moves.device.type != "cpu" or not moves.is_contiguous() or moves.numel() % 2:
+        raise ValueError("moves are pairs of 32-bit integers on the host, contiguous")
+    _check(_lib.mmaemu_cache_copy_pages(_address(memory), moves.data_ptr(), moves.numel() // 2, pages, page_bytes, layers, layer_bytes, _stream(stream) or 0))
 
 
 # ---- unpacking of the device-side result structs (host copies; no arithmetic) -----------

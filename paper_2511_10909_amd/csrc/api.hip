@@ -1,9 +1,10 @@
 // C-ABI entry points of libmmaemu: argument validation, error reporting, dispatch.
 // All validation happens here, on the host, before any kernel is enqueued.
-#include "common.hpp"
+#include "cache_fp4.hpp"
 
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 #include <new>
 
@@ -994,6 +995,146 @@ mmaemu_status mmaemu_matmul_fp4_kernel(uint32_t m, uint32_t n, uint32_t k, mmaem
     if (st != MMAEMU_OK) return st;
     *name = matmul_fp4_kernel_name(m, n, k, a_type, scale_format);
     return MMAEMU_OK;
+}
+
+} // extern "C"
+
+// what the calls on a cache share, but for pointers
+template <class Args> static mmaemu_status check_cache(const Args &a, const char *what)
+{
+    if (a.type != MMAEMU_BF16 && a.type != MMAEMU_FP16) { set_error("%s: type must be BF16 or FP16", what); return MMAEMU_ERR_UNSUPPORTED; }
+    if (a.dim != 64 && a.dim != 128) { set_error("%s: heads of 64 or 128 elements, not %u", what, a.dim); return MMAEMU_ERR_UNSUPPORTED; }
+    if (a.page_tokens == 0 || a.page_tokens % 32 || a.page_tokens > 65536) { set_error("%s: page_tokens=%u must be a multiple of 32 up to 65536", what, a.page_tokens); return MMAEMU_ERR_SHAPE; }
+    if (a.kv_heads == 0 || a.kv_heads > 1024 || a.heads > 4096) { set_error("%s: kv_heads 1 .. 1024, heads up to 4096", what); return MMAEMU_ERR_SHAPE; }
+    if (a.pages == 0 || a.pages > (1ull << 30)) { set_error("%s: pages outside 1 .. 2^30", what); return MMAEMU_ERR_SHAPE; }
+    if (a.tokens > (1ull << 30) || a.max_tokens > (1u << 24) || a.sequences > 65535) { set_error("%s: tokens above 2^30, max_tokens above 2^24 or sequences above 65535", what); return MMAEMU_ERR_SHAPE; }
+    if (a.table_stride == 0 || a.table_stride > 0x7FFFFFFFull / a.page_tokens) { set_error("%s: a row of the table must hold 1 .. 2^31 - 1 tokens", what); return MMAEMU_ERR_SHAPE; }
+    return MMAEMU_OK;
+}
+static bool is_row_stride(uint64_t &stride, uint64_t row)              // 0 becomes the row's length
+{
+    if (stride == 0) stride = row;
+    return stride >= row && stride <= (1ull << 32) && stride % 8 == 0;
+}
+template <class Args> static bool is_table(const Args &a, const char *what)
+{
+    if (a.cache && a.table && a.lengths && a.begins && !((uintptr_t)a.cache & 15) && !(((uintptr_t)a.table | (uintptr_t)a.lengths | (uintptr_t)a.begins) & 3)) return true;
+    set_error("%s: NULL cache, table, lengths or begins, or the cache not aligned to 16 bytes, the others to 4", what);
+    return false;
+}
+template <class Args> static CacheArgs cache_args(const Args &a)
+{
+    return {(uint8_t *)a.cache, a.table, a.lengths, a.begins, a.table_stride, (uint32_t)a.pages, a.kv_heads, a.page_tokens / 32, a.sequences, (uint32_t)a.tokens,
+            (uint32_t)(a.table_stride * a.page_tokens)};
+}
+
+extern "C" {
+
+mmaemu_status mmaemu_cache_append_fp4(const mmaemu_cache_append_fp4_args *args)
+{
+    const char *what = "cache_append_fp4";
+    if (!is_args(args, sizeof(*args), what)) return MMAEMU_ERR_INVALID_ARG;
+    mmaemu_cache_append_fp4_args a = *args;
+    const mmaemu_status st = check_cache(a, what);
+    if (st != MMAEMU_OK) return st;
+    if (a.weight_type != a.type && a.weight_type != MMAEMU_FP32) { set_error("%s: weight_type must be type or FP32", what); return MMAEMU_ERR_UNSUPPORTED; }
+    if (a.rotary_dim % 16 || a.rotary_dim > a.dim) { set_error("%s: rotary_dim=%u must be a multiple of 16 up to dim", what, a.rotary_dim); return MMAEMU_ERR_SHAPE; }
+    if ((uint64_t)a.max_tokens * (a.heads + 2 * a.kv_heads) > (1ull << 28)) { set_error("%s: max_tokens * (heads + 2 kv_heads) above 2^28", what); return MMAEMU_ERR_SHAPE; }
+    if (a.rotation_style > MMAEMU_ROTATE_PAIRS || a.scale_rule > MMAEMU_SCALE_RULE_FIT) { set_error("%s: rotation style or scale rule out of range", what); return MMAEMU_ERR_INVALID_ARG; }
+    if (!(a.eps >= 0.0) || a.eps > 1.7976931348623157e308) { set_error("%s: eps must be finite and not negative", what); return MMAEMU_ERR_INVALID_ARG; }
+    const uint64_t wide = (uint64_t)a.heads * a.dim, narrow = (uint64_t)a.kv_heads * a.dim;
+    if (!is_row_stride(a.q_stride, wide) || !is_row_stride(a.q_out_stride, wide) || !is_row_stride(a.k_stride, narrow) || !is_row_stride(a.v_stride, narrow)) {
+        set_error("%s: strides must be multiples of 8 from their row's length to 2^32", what);
+        return MMAEMU_ERR_SHAPE;
+    }
+    if (!a.q != !a.q_out || (a.q && a.heads == 0) || (!a.q && a.heads != 0 && a.tokens != 0)) { set_error("%s: q and q_out go together, with heads", what); return MMAEMU_ERR_INVALID_ARG; }
+    if (!a.k != !a.v || ((a.k_values || a.v_values) && !a.k)) { set_error("%s: k and v go together, and values with them", what); return MMAEMU_ERR_INVALID_ARG; }
+    if (a.q_out && a.q_out == a.q && a.q_stride != a.q_out_stride) { set_error("%s: q_out = q needs equal strides", what); return MMAEMU_ERR_INVALID_ARG; }
+    if (a.sequences == 0 || a.tokens == 0 || a.max_tokens == 0 || (!a.q && !a.k)) return MMAEMU_OK;
+    if (!is_table(a, what)) return MMAEMU_ERR_INVALID_ARG;
+    if (a.rotary_dim && !a.rotation) { set_error("%s: rotary_dim needs a rotation table", what); return MMAEMU_ERR_INVALID_ARG; }
+    const uintptr_t wmask = a.weight_type == MMAEMU_FP32 ? 3 : 1;
+    if ((((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.q_out | (uintptr_t)a.k_values | (uintptr_t)a.v_values) & 15) ||
+        (((uintptr_t)a.q_weight | (uintptr_t)a.k_weight) & wmask) || ((uintptr_t)a.rotation & 3)) {
+        set_error("%s: q, k, v and outputs must be aligned to 16 bytes, weights and rotation to their elements", what);
+        return MMAEMU_ERR_INVALID_ARG;
+    }
+    return launch_cache_append(a, cache_args(a), (hipStream_t)a.hip_stream);
+}
+
+static mmaemu_status check_attention(const mmaemu_attention_fp4_args &a)
+{
+    const mmaemu_status st = check_cache(a, "attention_fp4");
+    if (st != MMAEMU_OK) return st;
+    if (a.heads == 0 || a.heads % a.kv_heads) { set_error("attention_fp4: heads=%u must be a multiple of kv_heads=%u", a.heads, a.kv_heads); return MMAEMU_ERR_SHAPE; }
+    if ((uint64_t)a.max_tokens * (a.heads / a.kv_heads) > (1ull << 24) || (uint64_t)a.max_tokens * a.heads > (1ull << 28)) {
+        set_error("attention_fp4: max_tokens * heads / kv_heads above 2^24, or max_tokens * heads above 2^28");
+        return MMAEMU_ERR_SHAPE;
+    }
+    return MMAEMU_OK;
+}
+
+mmaemu_status mmaemu_attention_fp4_workspace(const mmaemu_attention_fp4_args *args, uint64_t *bytes)
+{
+    if (!is_args(args, sizeof(*args), "attention_fp4_workspace")) return MMAEMU_ERR_INVALID_ARG;
+    if (!bytes) { set_error("attention_fp4_workspace: NULL pointer"); return MMAEMU_ERR_INVALID_ARG; }
+    const mmaemu_status st = check_attention(*args);
+    if (st != MMAEMU_OK) return st;
+    *bytes = attention_fp4_workspace(*args);
+    return MMAEMU_OK;
+}
+
+mmaemu_status mmaemu_attention_fp4(const mmaemu_attention_fp4_args *args)
+{
+    const char *what = "attention_fp4";
+    if (!is_args(args, sizeof(*args), what)) return MMAEMU_ERR_INVALID_ARG;
+    mmaemu_attention_fp4_args a = *args;
+    const mmaemu_status st = check_attention(a);
+    if (st != MMAEMU_OK) return st;
+    if (!(a.scale >= 1e-30) || a.scale > 1e30) { set_error("%s: scale must lie in 1e-30 .. 1e30", what); return MMAEMU_ERR_INVALID_ARG; }
+    const uint64_t wide = (uint64_t)a.heads * a.dim;
+    if (!is_row_stride(a.q_stride, wide) || !is_row_stride(a.out_stride, wide)) { set_error("%s: strides must be multiples of 8 from their row's length to 2^32", what); return MMAEMU_ERR_SHAPE; }
+    if (a.out && a.out == a.q && a.q_stride != a.out_stride) { set_error("%s: out = q needs equal strides", what); return MMAEMU_ERR_INVALID_ARG; }
+    if (a.sequences == 0 || a.tokens == 0 || a.max_tokens == 0) return MMAEMU_OK;
+    if (!a.q || !a.out || (((uintptr_t)a.q | (uintptr_t)a.out) & 15)) { set_error("%s: q or out NULL or not aligned to 16 bytes", what); return MMAEMU_ERR_INVALID_ARG; }
+    if (!is_table(a, what)) return MMAEMU_ERR_INVALID_ARG;
+    const uint64_t bytes = attention_fp4_workspace(a);
+    if (bytes && (!a.workspace || ((uintptr_t)a.workspace & 15) || a.workspace_bytes < bytes)) {
+        set_error("%s: a workspace of %llu bytes, aligned to 16, is needed", what, (unsigned long long)bytes);
+        return MMAEMU_ERR_INVALID_ARG;
+    }
+    return launch_attention_fp4(a, cache_args(a), (hipStream_t)a.hip_stream);
+}
+
+mmaemu_status mmaemu_cache_copy_pages(void *memory, const int32_t *moves, uint64_t count, uint64_t pages, uint64_t page_bytes, uint64_t layers, uint64_t layer_bytes,
+                                      void *hip_stream)
+{
+    const char *what = "cache_copy_pages";
+    if (pages == 0 || pages > (1ull << 30) || page_bytes == 0 || page_bytes % 16 || page_bytes > (1ull << 32) || layers > 65535) {
+        set_error("%s: pages 1 .. 2^30, page_bytes a multiple of 16 up to 2^32, layers up to 65535", what);
+        return MMAEMU_ERR_SHAPE;
+    }
+    if (layer_bytes == 0) layer_bytes = pages * page_bytes;
+    if (layer_bytes < pages * page_bytes || layer_bytes % 16 || layer_bytes > (1ull << 46)) { set_error("%s: layer_bytes below a layer's pages, no multiple of 16 or above 2^46", what); return MMAEMU_ERR_SHAPE; }
+    if (count == 0 || layers == 0) return MMAEMU_OK;
+    if (!memory || ((uintptr_t)memory & 15) || !moves || ((uintptr_t)moves & 3)) { set_error("%s: NULL memory or moves, or memory not aligned to 16 bytes", what); return MMAEMU_ERR_INVALID_ARG; }
+    for (uint64_t i = 0; i < 2 * count; ++i)
+        if (moves[i] < 0 || (uint64_t)moves[i] >= pages) { set_error("%s: move %llu names page %d of %llu", what, (unsigned long long)(i / 2), moves[i], (unsigned long long)pages); return MMAEMU_ERR_INVALID_ARG; }
+    // a bit for each page that is a target, and one for each that is a source
+    uint64_t *bits = (uint64_t *)calloc(pages / 32 + 1, sizeof(uint64_t));
+    if (!bits) { set_error("%s: no host memory for %llu pages", what, (unsigned long long)pages); return MMAEMU_ERR_NOMEM; }
+    bool fine = true;
+    for (uint64_t i = 0; i < count && fine; ++i) {
+        const uint32_t from = (uint32_t)moves[2 * i], to = (uint32_t)moves[2 * i + 1];
+        if (from == to) continue;
+        fine = !(bits[to / 32] >> (2 * (to % 32)) & 1);
+        bits[to / 32] |= 1ull << (2 * (to % 32));
+        bits[from / 32] |= 2ull << (2 * (from % 32));
+    }
+    for (uint64_t i = 0; i < count && fine; ++i) fine = moves[2 * i] == moves[2 * i + 1] || (bits[moves[2 * i + 1] / 32] >> (2 * (moves[2 * i + 1] % 32)) & 3) == 1;
+    free(bits);
+    if (!fine) { set_error("%s: a page is the target of two moves, or the target of one and the source of another", what); return MMAEMU_ERR_INVALID_ARG; }
+    return launch_cache_copy(memory, moves, count, page_bytes, layers, layer_bytes, (hipStream_t)hip_stream);
 }
 
 } // extern "C"

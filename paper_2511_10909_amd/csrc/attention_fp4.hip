@@ -1,0 +1,421 @@
+// Attention over the cache in 4 bits: out = softmax(scale q K^T) V over the tokens that a row sees, from one token to prompts.
+//
+// The rows of a KV head are its group's query heads of all the call's tokens of a sequence, r = token * group + head: they share K and V.  One pass
+// over the tokens with a running maximum m and sum l per row, in units of log2:
+//   s = scale log2(e) q.k;  m' = max(m, max s);  p = 2^(s - m');  l = l 2^(m - m') + sum p;  O = O 2^(m - m') + p V;  out = O / l
+// Both products are 16 x 16 x 32 instructions on operands that lie in the cache as the lanes take them (cache_fp4.hpp), brought to 16 bits, which is
+// exact: K to the queries' type, V to FP16.  The scores' registers are the second product's operand as they are, rounded to FP16 after a shift by 2^10:
+// weights down to 2^-24 of the largest keep all their bits.
+#include "cache_fp4.hpp"
+#include "fp4_operands.hpp"
+
+namespace mmaemu {
+
+struct AttentionArgs {
+    CacheArgs c;
+    const void *q;
+    void *out;
+    float *part;                                   // [split][token][head][D], unnormalised, and behind them
+    f32x2 *stat;                                   // [split][token][head] (m, l)
+    uint64_t q_stride, out_stride;
+    uint32_t heads, group, max_tokens, window, splits, blocks;         // blocks: of rows, of a sequence's KV head
+    float c2;                                      // scale log2(e)
+};
+
+constexpr float LOWEST = -3.0e38f;                 // a maximum over nothing
+constexpr float SHIFT = 10.0f;                     // weights are held times 2^SHIFT
+
+// The granules that the rows r0 .. of a block see, and the part of them that a split takes.
+struct Range { uint32_t first, count, chunk; };
+__device__ __forceinline__ Range granules_of(const AttentionArgs &a, const Sequence &sq, uint32_t r0, uint32_t rows, uint32_t least)
+{
+    const uint32_t all = (sq.n < a.max_tokens ? sq.n : a.max_tokens) * a.group;
+    const uint32_t last = (r0 + rows < all ? r0 + rows : all) - 1;
+    const int32_t p0 = sq.start + (int32_t)(r0 / a.group), end = sq.start + (int32_t)(last / a.group) + 1;
+    const int32_t begin = a.window && (uint32_t)(p0 < 0 ? 0 : p0) >= a.window ? p0 + 1 - (int32_t)a.window : 0;
+    Range g;
+    g.first = (uint32_t)begin / 32u;
+    g.count = end > begin ? ((uint32_t)end + 31u) / 32u - g.first : 0u;
+    const uint32_t even = (g.count + a.splits - 1) / a.splits;
+    g.chunk = even > least ? even : least;
+    return g;
+}
+
+__device__ __forceinline__ float other_rows_max(float x)               // over lanes l, l + 16, l + 32, l + 48
+{
+    const uint32_t b = __float_as_uint(x);
+    const auto p = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    const float y = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    const uint32_t c = __float_as_uint(y);
+    const auto q = __builtin_amdgcn_permlane16_swap(c, c, false, false);
+    return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+__device__ __forceinline__ float other_rows_sum(float x)
+{
+    const uint32_t b = __float_as_uint(x);
+    const auto p = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    const float y = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    const uint32_t c = __float_as_uint(y);
+    const auto q = __builtin_amdgcn_permlane16_swap(c, c, false, false);
+    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
+// a granule as a lane holds it
+template <int D> struct Granule {
+    u32x4 k[D / 64], v[D / 64];
+    uint32_t ks;                                   // its K scales of both halves
+    uint32_t vs[2];                                // its V scales of eight tokens
+};
+template <int D> __device__ __forceinline__ Granule<D> load_granule(const uint8_t *at, uint32_t lane)
+{
+    const uint32_t g = lane >> 4, l = lane & 15u;
+    constexpr uint32_t B = D / 32;
+    Granule<D> x;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+        x.k[i] = *reinterpret_cast<const u32x4 *>(at + 1024 * i + 16 * lane);
+        x.v[i] = *reinterpret_cast<const u32x4 *>(at + 16 * D + 1024 * i + 16 * lane);
+    }
+    x.ks = *reinterpret_cast<const uint16_t *>(at + 32 * D + (g * B / 4 * 16 + l) * 2);
+    const uint32_t *vs = reinterpret_cast<const uint32_t *>(at + 33 * D + (g * B + l * B / 16) * 8);
+    x.vs[0] = vs[0];
+    x.vs[1] = vs[1];
+    return x;
+}
+
+// the 16-bit K operand of half a, dimensions 8 j .. 8 j + 7 of the lane's D / 4
+template <int T, int D> __device__ __forceinline__ Frag16 k_operand(const Granule<D> &x, int a, int j)
+{
+    const uint32_t word = D == 128 ? x.k[D == 128 ? a : 0][j] : x.k[0][2 * a + j];
+    const uint32_t code = a ? x.ks >> 8 : x.ks & 0xFFu;
+    return T == MMAEMU_BF16 ? weights_bf16(word, code) : weights_fp16(word, code);
+}
+
+// codes of bytes 0xFF in a word, as 0x80 in their bytes (exact: the lowest byte that is one is found, and those above it)
+__device__ __forceinline__ uint32_t any_nan_code(uint32_t w) { return (~w - 0x01010101u) & w & 0x80808080u; }
+
+// Rows of NR x 16 x ROW_WAVES, tokens split over the other wavefronts of four.
+template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__(256) attention_kernel(const AttentionArgs a)
+{
+    constexpr uint32_t WAVES = 4, TOKEN_WAVES = WAVES / ROW_WAVES, J = D / 32, DT = D / 16;
+    constexpr uint32_t ROWS = 16 * NR * ROW_WAVES;
+    __shared__ __attribute__((aligned(16))) float lds[TOKEN_WAVES > 1 ? TOKEN_WAVES * 16 * NR * (D + 4) : 1];
+    __shared__ f32x2 lds_stat[TOKEN_WAVES > 1 ? TOKEN_WAVES * 16 * NR : 1];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15u;
+    const uint32_t head = blockIdx.x % a.c.kv_heads, block = a.blocks - 1 - blockIdx.x / a.c.kv_heads;        // the longest rows first
+    const uint32_t split = blockIdx.y, s = blockIdx.z;
+    const Sequence sq = sequence_of(a.c, s);
+    const uint32_t rows = (sq.n < a.max_tokens ? sq.n : a.max_tokens) * a.group;
+    if (block * ROWS >= rows) return;
+    const Range range = granules_of(a, sq, block * ROWS, ROWS, 2 * TOKEN_WAVES);
+    const uint32_t begin = split * range.chunk;
+    if (a.splits > 1 && begin >= range.count) return;
+    const uint32_t count = range.count > begin ? (range.count - begin < range.chunk ? range.count - begin : range.chunk) : 0u;
+    const uint32_t r0 = block * ROWS + (ROW_WAVES > 1 ? wave * 16 * NR : 0);
+
+    // this lane's rows: query operands, and positions (rows that are not there: the last one again)
+    Frag16 q[NR][J];
+    int32_t pos[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        const uint32_t r = r0 + 16 * i + l < rows ? r0 + 16 * i + l : rows - 1, token = r / a.group, h = r % a.group;
+        pos[i] = sq.start + (int32_t)token;
+        const uint16_t *from = (const uint16_t *)a.q + (uint64_t)(sq.first + token) * a.q_stride + (uint64_t)(head * a.group + h) * D + g * (D / 4);
+#pragma unroll
+        for (uint32_t j = 0; j < J; ++j) q[i][j].w = *reinterpret_cast<const u32x4 *>(from + 8 * j);
+    }
+    // positions of the wavefront's first and last rows
+    const uint32_t r_last = (r0 + 16 * NR < rows ? r0 + 16 * NR : rows) - 1;
+    const int32_t pos_first = sq.start + (int32_t)(r0 / a.group), pos_last = r0 < rows ? sq.start + (int32_t)(r_last / a.group) : -1;
+
+    float m[NR], sum[NR];
+    f32x4 acc[NR][DT];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        m[i] = LOWEST;
+        sum[i] = 0.0f;
+#pragma unroll
+        for (uint32_t d = 0; d < DT; ++d) acc[i][d] = f32x4{0, 0, 0, 0};
+    }
+
+    for (uint32_t n = ROW_WAVES > 1 ? 0 : wave; n < count; n += TOKEN_WAVES) {
+        const uint32_t granule = range.first + begin + n;
+        const int32_t t0 = (int32_t)(32 * granule);
+        if (t0 > pos_last) break;
+        const int32_t page = a.c.table[s * a.c.table_stride + granule / a.c.page_granules];
+        const uint8_t *at = granule_at<D>(a.c, page, head, granule % a.c.page_granules);
+        if (!at) continue;
+        Granule<D> x = load_granule<D>(at, lane);
+        // whether all rows see all of the granule
+        const bool whole = t0 + 31 <= pos_first && (!a.window || (uint32_t)(pos_last - t0) < a.window);
+        if (!whole) {
+            // tokens that no row sees may hold anything: their V scales become the least
+            const int32_t t = t0 + 8 * (int32_t)g;
+            const int32_t low = a.window && (uint32_t)(pos_first < 0 ? 0 : pos_first) >= a.window ? pos_first + 1 - (int32_t)a.window : 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (t + e > pos_last || t + e < low) x.vs[e / 4] &= ~(0xFFu << (8 * (e % 4)));
+        }
+        // scores: half a, register e is token 8 g + 4 a + e
+        f32x4 sc[NR][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < NR; ++i) sc[i][h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (uint32_t j = 0; j < J; ++j) {
+                const Frag16 k = k_operand<T, D>(x, h, (int)j);
+#pragma unroll
+                for (int i = 0; i < NR; ++i) sc[i][h] = T == MMAEMU_BF16 ? mfma_bf16(k, q[i][j], sc[i][h]) : mfma_fp16(k, q[i][j], sc[i][h]);
+            }
+        }
+        Frag16 p[NR];
+        f16x8 seen[NR];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            float top = LOWEST, z[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                z[e] = sc[i][e / 4][e % 4] * a.c2;
+                if (!whole) {
+                    const int32_t t = t0 + 8 * (int32_t)g + e;
+                    const bool sees = t <= pos[i] && (!a.window || (uint32_t)(pos[i] - t) < a.window);
+                    z[e] = sees ? z[e] : -__builtin_inff();
+                    seen[i][e] = sees ? (_Float16)1.0f : (_Float16)0.0f;
+                } else seen[i][e] = (_Float16)1.0f;
+                top = fmaxf(top, z[e]);
+            }
+            top = fmaxf(m[i], other_rows_max(top));
+            const float factor = __builtin_amdgcn_exp2f(m[i] - top);
+            m[i] = top;
+            sum[i] *= factor;
+#pragma unroll
+            for (uint32_t d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][d][e] *= factor;
+            f16x8 w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float y = __builtin_amdgcn_exp2f(z[e] - top + SHIFT);
+                sum[i] += y;
+                w[e] = (_Float16)y;
+            }
+            p[i].w = __builtin_bit_cast(u32x4, w);
+        }
+        // NaN blocks among the values: they are taken as zeros, and make NaN the outputs of the rows that see them
+        if (__any(any_nan_code(x.vs[0]) | any_nan_code(x.vs[1]))) {
+            f16x8 bad;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool nan = (x.vs[e / 4] >> (8 * (e % 4)) & 0xFFu) == 0xFFu;
+                bad[e] = nan ? (_Float16)1.0f : (_Float16)0.0f;
+                if (nan) x.vs[e / 4] &= ~(0xFFu << (8 * (e % 4)));
+            }
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad, seen[i], f32x4{0, 0, 0, 0}, 0, 0, 0);
+#pragma unroll
+                for (uint32_t d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][d][e] = hit[e] > 0.0f ? __builtin_nanf("") : acc[i][d][e];
+            }
+        }
+        // values: word pairs of two elements 2 c, 2 c + 1 and eight tokens
+#pragma unroll
+        for (uint32_t c = 0; c < DT / 2; ++c) {
+            const uint32_t w0 = x.v[c / 2][2 * (c % 2)], w1 = x.v[c / 2][2 * (c % 2) + 1];
+            f16x2 y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float unit = __uint_as_float((x.vs[e / 4] >> (8 * (e % 4)) & 0xFFu) << 23);
+                const uint32_t w = e < 4 ? w0 : w1;
+                y[e] = e % 4 == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit, 0) : e % 4 == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit, 1) :
+                       e % 4 == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit, 2) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit, 3);
+            }
+            Frag16 even, odd;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t lo = __builtin_bit_cast(uint32_t, y[2 * e]), hi = __builtin_bit_cast(uint32_t, y[2 * e + 1]);
+                even.w[e] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+                odd.w[e] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+            }
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                acc[i][2 * c] = mfma_fp16(even, p[i], acc[i][2 * c]);
+                acc[i][2 * c + 1] = mfma_fp16(odd, p[i], acc[i][2 * c + 1]);
+            }
+        }
+    }
+
+#pragma unroll
+    for (int i = 0; i < NR; ++i) sum[i] = other_rows_sum(sum[i]);
+
+    // one row's D / 16 outputs of register e, elements (4 g + e) D / 16 ..
+    const auto store = [&](uint32_t r, uint32_t e, const float (&o)[DT], float rm, float rl) MMAEMU_INLINE {
+        if (r >= rows) return;
+        const uint64_t token = sq.first + r / a.group;
+        const uint32_t h = head * a.group + r % a.group, at = (4 * g + e) * DT;
+        if (a.splits > 1) {
+            const uint64_t row = ((uint64_t)split * a.c.tokens + token) * a.heads + h;
+            float *to = a.part + row * D + at;
+#pragma unroll
+            for (uint32_t d = 0; d < DT; d += 4) *reinterpret_cast<f32x4 *>(to + d) = f32x4{o[d], o[d + 1], o[d + 2], o[d + 3]};
+            if (e == 0 && g == 0) a.stat[row] = f32x2{rm, rl};
+            return;
+        }
+        const float inverse = rl == 0.0f ? 0.0f : 1.0f / rl;
+        uint16_t *to = (uint16_t *)a.out + token * a.out_stride + (uint64_t)h * D + at;
+        uint32_t w[DT / 2];
+#pragma unroll
+        for (uint32_t d = 0; d < DT; d += 2) w[d / 2] = float_elem<T>(o[d] * inverse) | float_elem<T>(o[d + 1] * inverse) << 16;
+        if constexpr (DT == 8) *reinterpret_cast<u32x4 *>(to) = u32x4{w[0], w[1], w[2], w[3]};
+        else {
+            Words2<8> v;
+            v.w[0] = w[0];
+            v.w[1] = w[1];
+            *reinterpret_cast<Words2<8> *>(to) = v;
+        }
+    };
+
+    if constexpr (TOKEN_WAVES == 1) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                float o[DT];
+#pragma unroll
+                for (uint32_t d = 0; d < DT; ++d) o[d] = acc[i][d][e];
+                store(r0 + 16 * i + l, e, o, m[i], sum[i]);
+            }
+    } else {
+        // the wavefronts' parts of the same rows meet in LDS: rows are D + 4 numbers apart
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+            if (g == 0) lds_stat[wave * 16 * NR + 16 * i + l] = f32x2{m[i], sum[i]};
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            float top = LOWEST;
+#pragma unroll
+            for (uint32_t w = 0; w < TOKEN_WAVES; ++w) top = fmaxf(top, lds_stat[w * 16 * NR + 16 * i + l][0]);
+            const float factor = __builtin_amdgcn_exp2f(m[i] - top);
+            float *to = lds + (wave * 16 * NR + 16 * i + l) * (D + 4);
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+#pragma unroll
+                for (uint32_t d = 0; d < DT; d += 4)
+                    *reinterpret_cast<f32x4 *>(to + (4 * g + e) * DT + d) = f32x4{acc[i][d][e] * factor, acc[i][d + 1][e] * factor, acc[i][d + 2][e] * factor, acc[i][d + 3][e] * factor};
+        }
+        __syncthreads();
+        // wavefront w joins register e = w of all
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            float top = LOWEST, total = 0.0f, o[DT];
+#pragma unroll
+            for (uint32_t w = 0; w < TOKEN_WAVES; ++w) top = fmaxf(top, lds_stat[w * 16 * NR + 16 * i + l][0]);
+#pragma unroll
+            for (uint32_t w = 0; w < TOKEN_WAVES; ++w) {
+                const f32x2 st = lds_stat[w * 16 * NR + 16 * i + l];
+                total += st[1] * __builtin_amdgcn_exp2f(st[0] - top);
+            }
+#pragma unroll
+            for (uint32_t d = 0; d < DT; d += 4) {
+                f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+                for (uint32_t w = 0; w < TOKEN_WAVES; ++w) v += *reinterpret_cast<const f32x4 *>(lds + (w * 16 * NR + 16 * i + l) * (D + 4) + (4 * g + wave) * DT + d);
+                o[d] = v[0]; o[d + 1] = v[1]; o[d + 2] = v[2]; o[d + 3] = v[3];
+            }
+            const uint32_t r = r0 + 16 * i + l;
+            store(r, wave, o, top, total);
+        }
+    }
+}
+
+// The splits' parts of a row, joined: a wavefront per row.
+template <int T, int D> __global__ void __launch_bounds__(256) attention_join_kernel(const AttentionArgs a, uint32_t block_rows, uint32_t least)
+{
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint32_t r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);              // row: token, then head
+    const Sequence sq = sequence_of(a.c, blockIdx.y);
+    const uint32_t n = sq.n < a.max_tokens ? sq.n : a.max_tokens, i = r / a.heads, h = r % a.heads;
+    if (i >= n) return;
+    const uint32_t in_head = i * a.group + h % a.group;
+    const Range range = granules_of(a, sq, in_head / block_rows * block_rows, block_rows, least);
+    const uint32_t parts = (range.count + range.chunk - 1) / range.chunk;          // at most 64
+    const uint64_t row = (uint64_t)(sq.first + i) * a.heads + h, apart = (uint64_t)a.c.tokens * a.heads;
+    f32x2 st = {LOWEST, 0.0f};
+    if (lane < parts) st = a.stat[lane * apart + row];
+    float top = st[0];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    const float factor = __builtin_amdgcn_exp2f(st[0] - top);
+    float total = st[1] * factor;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+    float o[D / 64] = {};
+    for (uint32_t z = 0; z < parts; ++z) {
+        const float f = __shfl(factor, (int)z);
+        const float *from = a.part + (z * apart + row) * D + lane * (D / 64);
+#pragma unroll
+        for (int d = 0; d < D / 64; ++d) o[d] += f * from[d];
+    }
+    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+    uint16_t *to = (uint16_t *)a.out + (uint64_t)(sq.first + i) * a.out_stride + (uint64_t)h * D + lane * (D / 64);
+    if constexpr (D == 128) *reinterpret_cast<uint32_t *>(to) = float_elem<T>(o[0] * inverse) | float_elem<T>(o[1] * inverse) << 16;
+    else *to = (uint16_t)float_elem<T>(o[0] * inverse);
+}
+
+// ---- which shape, and how many splits ------------------------------------------------------
+struct Plan { uint32_t nr, row_waves, block_rows, blocks, splits, least; };
+
+static Plan plan_of(const mmaemu_attention_fp4_args &a)
+{
+    const uint32_t rows = a.max_tokens * (a.heads / a.kv_heads);
+    Plan p;
+    p.nr = rows <= 16 ? 1 : 2;
+    p.row_waves = rows <= 64 ? 1 : 4;
+    p.block_rows = 16 * p.nr * p.row_waves;
+    p.blocks = (rows + p.block_rows - 1) / p.block_rows;
+    p.least = 2 * (4 / p.row_waves);
+    const uint64_t groups = (uint64_t)p.blocks * a.kv_heads * a.sequences;
+    const uint64_t seen = a.window && (uint64_t)a.window + a.max_tokens < a.max_length ? (uint64_t)a.window + a.max_tokens : a.max_length;
+    const uint64_t most = (seen + 31) / 32 / p.least;
+    uint64_t splits = groups ? 1024 / groups : 1;
+    if (splits > most) splits = most;
+    p.splits = splits < 1 ? 1 : splits > 64 ? 64 : (uint32_t)splits;
+    return p;
+}
+
+uint64_t attention_fp4_workspace(const mmaemu_attention_fp4_args &a)
+{
+    if (!a.sequences || !a.tokens || !a.max_tokens) return 0;
+    const Plan p = plan_of(a);
+    return p.splits > 1 ? (uint64_t)p.splits * a.tokens * a.heads * (a.dim + 2) * 4 : 0;
+}
+
+template <int T, int D> static mmaemu_status launch_typed(const AttentionArgs &p, const Plan &plan, hipStream_t s)
+{
+    const dim3 grid(plan.blocks * p.c.kv_heads, plan.splits, p.c.sequences);
+    if (plan.row_waves == 4) hipLaunchKernelGGL((attention_kernel<T, D, 2, 4>), grid, dim3(256), 0, s, p);
+    else if (plan.nr == 2) hipLaunchKernelGGL((attention_kernel<T, D, 2, 1>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((attention_kernel<T, D, 1, 1>), grid, dim3(256), 0, s, p);
+    MMAEMU_HIP(hipGetLastError());
+    if (plan.splits > 1) {
+        const uint64_t rows = (uint64_t)p.max_tokens * p.heads;
+        hipLaunchKernelGGL((attention_join_kernel<T, D>), dim3((uint32_t)((rows + 3) / 4), p.c.sequences), dim3(256), 0, s, p, plan.block_rows, plan.least);
+        MMAEMU_HIP(hipGetLastError());
+    }
+    return MMAEMU_OK;
+}
+
+mmaemu_status launch_attention_fp4(const mmaemu_attention_fp4_args &a, const CacheArgs &c, hipStream_t s)
+{
+    const Plan plan = plan_of(a);
+    AttentionArgs p = {c, a.q, a.out, (float *)a.workspace, nullptr, a.q_stride, a.out_stride, a.heads, a.heads / a.kv_heads, a.max_tokens, a.window, plan.splits,
+                       plan.blocks, (float)(a.scale * 1.4426950408889634)};
+    p.stat = (f32x2 *)(p.part + (uint64_t)plan.splits * a.tokens * a.heads * a.dim);
+    if (a.type == MMAEMU_BF16) return a.dim == 128 ? launch_typed<MMAEMU_BF16, 128>(p, plan, s) : launch_typed<MMAEMU_BF16, 64>(p, plan, s);
+    return a.dim == 128 ? launch_typed<MMAEMU_FP16, 128>(p, plan, s) : launch_typed<MMAEMU_FP16, 64>(p, plan, s);
+}
+
+} // namespace mmaemu

@@ -140,6 +140,16 @@ template <int EMAX, uint32_t TOPMAN> __device__ __forceinline__ uint32_t e8m0_co
 // 2^(127 - code), which takes a block to its elements' range (code at most 253); 0 for the NaN code: no element is read then
 __device__ __forceinline__ float e8m0_inverse(uint32_t code) { return code == 0xFFu ? 0.0f : __uint_as_float((254u - code) << 23); }
 
+// eight values to packed E2M1 codes, nearest even, saturated
+__device__ __forceinline__ uint32_t pack_fp4(const float (&f)[8])
+{
+    uint32_t q = 0;
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[0], f[1], 1.0f, 0);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[2], f[3], 1.0f, 1);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[4], f[5], 1.0f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[6], f[7], 1.0f, 3);
+}
+
 // ---- reductions over lanes by DPP ---------------------------------------------------------
 template <int CTRL> __device__ __forceinline__ uint32_t dpp_max(uint32_t x)
 {

@@ -26,15 +26,6 @@ struct QuantArgs {
 
 constexpr int QUANT_UNROLL = 4;
 
-__device__ __forceinline__ uint32_t pack_fp4(const float (&f)[8])
-{
-    uint32_t q = 0;
-    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[0], f[1], 1.0f, 0);
-    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[2], f[3], 1.0f, 1);
-    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[4], f[5], 1.0f, 2);
-    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[6], f[7], 1.0f, 3);
-}
-
 // x / d, correctly rounded: the product with the rounded inverse, corrected by its exact remainder
 __device__ __forceinline__ double quotient(double x, double d, double inverse)
 {

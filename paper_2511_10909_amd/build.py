@@ -15,7 +15,8 @@ COMMON = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-I", os.path.j
           # no packed-FP32 vector forms: some of them have given wrong results now and then
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # the NORMAL generator is defined as a fixed sequence of IEEE operations: no fused multiply-add
-PER_FILE = {"gen.hip": ["-ffp-contract=off"], "emulate_addmul.hip": ["-ffp-contract=off"]}
+# (cache_append_fp4: a contraction would round binary64 results to 16 bits at once, past binary32)
+PER_FILE = {"cache_append_fp4.hip": ["-ffp-contract=off"], "gen.hip": ["-ffp-contract=off"], "emulate_addmul.hip": ["-ffp-contract=off"]}
 
 
 def sources():

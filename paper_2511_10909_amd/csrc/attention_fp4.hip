@@ -23,7 +23,7 @@ struct AttentionArgs {
 };
 
 constexpr float LOWEST = -3.0e38f;                 // a maximum over nothing
-constexpr float SHIFT = 10.0f;                     // weights are held times 2^SHIFT
+constexpr float SHIFT = 10.0f, LAG = 5.0f;         // weights are held times 2^SHIFT; how far (in log2) a maximum may fall behind
 
 // The granules that the rows r0 .. of a block see, and the part of them that a split takes.
 struct Range { uint32_t first, count, chunk; };
@@ -49,15 +49,6 @@ __device__ __forceinline__ float other_rows_max(float x)               // over l
     const uint32_t c = __float_as_uint(y);
     const auto q = __builtin_amdgcn_permlane16_swap(c, c, false, false);
     return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
-}
-__device__ __forceinline__ float other_rows_sum(float x)
-{
-    const uint32_t b = __float_as_uint(x);
-    const auto p = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-    const float y = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    const uint32_t c = __float_as_uint(y);
-    const auto q = __builtin_amdgcn_permlane16_swap(c, c, false, false);
-    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
 // a granule as a lane holds it
@@ -94,13 +85,35 @@ template <int T, int D> __device__ __forceinline__ Frag16 k_operand(const Granul
 // codes of bytes 0xFF in a word, as 0x80 in their bytes (exact: the lowest byte that is one is found, and those above it)
 __device__ __forceinline__ uint32_t any_nan_code(uint32_t w) { return (~w - 0x01010101u) & w & 0x80808080u; }
 
-// Rows of NR x 16 x ROW_WAVES, tokens split over the other wavefronts of four.
-template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__(256) attention_kernel(const AttentionArgs a)
+// The pages of a wavefront's granules: granules `at`, `at` + step, ... of the sequence, 64 entries of the table at a time, one a lane.
+template <int D> struct Walk {
+    const uint8_t *base;                           // of the head in page 0
+    const int32_t *row;
+    uint64_t page_bytes;
+    uint32_t pages, page_granules, at, step, lane;
+    int32_t entry;
+    __device__ __forceinline__ Walk(const CacheArgs &c, uint32_t sequence, uint32_t head, uint32_t first, uint32_t step_, uint32_t lane_)
+        : base(c.cache + (uint64_t)head * c.page_granules * (34 * D)), row(c.table + sequence * c.table_stride), page_bytes((uint64_t)c.kv_heads * c.page_granules * (34 * D)),
+          pages(c.pages), page_granules(c.page_granules), at(first), step(step_), lane(lane_), entry(-1) {}
+    // the entries for the next 64 of the `left` granules still to come
+    __device__ __forceinline__ void refill(uint32_t n, uint32_t left) { entry = lane < left ? row[(at + (n + lane) * step) / page_granules] : -1; }
+    // granule n of the walk; NULL where its page is none
+    __device__ __forceinline__ const uint8_t *granule(uint32_t n) const
+    {
+        const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(entry, (int)(n & 63u)), g = (at + n * step) % page_granules;
+        return page < pages ? base + page * page_bytes + g * (34 * D) : nullptr;
+    }
+};
+
+// Rows of NR x 16 x ROW_WAVES, tokens split over the other wavefronts of four.  Where the tiles of rows are many, the queries wait in LDS.
+template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) attention_kernel(const AttentionArgs a)
 {
     constexpr uint32_t WAVES = 4, TOKEN_WAVES = WAVES / ROW_WAVES, J = D / 32, DT = D / 16;
     constexpr uint32_t ROWS = 16 * NR * ROW_WAVES;
+    constexpr bool Q_LDS = NR >= 4;
     __shared__ __attribute__((aligned(16))) float lds[TOKEN_WAVES > 1 ? TOKEN_WAVES * 16 * NR * (D + 4) : 1];
     __shared__ f32x2 lds_stat[TOKEN_WAVES > 1 ? TOKEN_WAVES * 16 * NR : 1];
+    __shared__ u32x4 lds_q[Q_LDS ? WAVES * NR * J * 64 : 1];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15u;
     const uint32_t head = blockIdx.x % a.c.kv_heads, block = a.blocks - 1 - blockIdx.x / a.c.kv_heads;        // the longest rows first
     const uint32_t split = blockIdx.y, s = blockIdx.z;
@@ -110,44 +123,64 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
     const Range range = granules_of(a, sq, block * ROWS, ROWS, 2 * TOKEN_WAVES);
     const uint32_t begin = split * range.chunk;
     if (a.splits > 1 && begin >= range.count) return;
-    const uint32_t count = range.count > begin ? (range.count - begin < range.chunk ? range.count - begin : range.chunk) : 0u;
+    uint32_t count = range.count > begin ? (range.count - begin < range.chunk ? range.count - begin : range.chunk) : 0u;
     const uint32_t r0 = block * ROWS + (ROW_WAVES > 1 ? wave * 16 * NR : 0);
+    // positions of the wavefront's first and last rows; its granules
+    const uint32_t r_last = (r0 + 16 * NR < rows ? r0 + 16 * NR : rows) - 1;
+    const int32_t pos_first = sq.start + (int32_t)(r0 / a.group), pos_last = r0 < rows ? sq.start + (int32_t)(r_last / a.group) : -1;
+    const uint32_t ends = pos_last < 0 ? 0u : (uint32_t)pos_last / 32u + 1, from = range.first + begin;
+    if (ROW_WAVES > 1) count = ends > from ? (ends - from < count ? ends - from : count) : 0u;
+    const uint32_t skip = ROW_WAVES > 1 ? 0 : wave, mine = count > skip ? (count - skip + TOKEN_WAVES - 1) / TOKEN_WAVES : 0u;
+    Walk<D> walk(a.c, s, head, from + skip, TOKEN_WAVES, lane);
+    walk.refill(0, mine);
 
     // this lane's rows: query operands, and positions (rows that are not there: the last one again)
-    Frag16 q[NR][J];
+    Frag16 q[Q_LDS ? 1 : NR][J];
+    u32x4 *const wave_q = lds_q + wave * (NR * J * 64) + lane;
     int32_t pos[NR];
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const uint32_t r = r0 + 16 * i + l < rows ? r0 + 16 * i + l : rows - 1, token = r / a.group, h = r % a.group;
         pos[i] = sq.start + (int32_t)token;
-        const uint16_t *from = (const uint16_t *)a.q + (uint64_t)(sq.first + token) * a.q_stride + (uint64_t)(head * a.group + h) * D + g * (D / 4);
+        const uint16_t *at = (const uint16_t *)a.q + (uint64_t)(sq.first + token) * a.q_stride + (uint64_t)(head * a.group + h) * D + g * (D / 4);
 #pragma unroll
-        for (uint32_t j = 0; j < J; ++j) q[i][j].w = *reinterpret_cast<const u32x4 *>(from + 8 * j);
+        for (uint32_t j = 0; j < J; ++j) {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(at + 8 * j);
+            if constexpr (Q_LDS) wave_q[(i * J + j) * 64] = w;         // (read by the lane that wrote it)
+            else q[i][j].w = w;
+        }
     }
-    // positions of the wavefront's first and last rows
-    const uint32_t r_last = (r0 + 16 * NR < rows ? r0 + 16 * NR : rows) - 1;
-    const int32_t pos_first = sq.start + (int32_t)(r0 / a.group), pos_last = r0 < rows ? sq.start + (int32_t)(r_last / a.group) : -1;
 
-    float m[NR], sum[NR];
-    f32x4 acc[NR][DT];
+    const Frag16 ones = {{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u}};
+    float m[NR];
+    f32x4 acc[NR][DT], sum[NR];                    // (a sum is in all four)
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         m[i] = LOWEST;
-        sum[i] = 0.0f;
+        sum[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (uint32_t d = 0; d < DT; ++d) acc[i][d] = f32x4{0, 0, 0, 0};
     }
 
-    for (uint32_t n = ROW_WAVES > 1 ? 0 : wave; n < count; n += TOKEN_WAVES) {
-        const uint32_t granule = range.first + begin + n;
-        const int32_t t0 = (int32_t)(32 * granule);
-        if (t0 > pos_last) break;
-        const int32_t page = a.c.table[s * a.c.table_stride + granule / a.c.page_granules];
-        const uint8_t *at = granule_at<D>(a.c, page, head, granule % a.c.page_granules);
-        if (!at) continue;
-        Granule<D> x = load_granule<D>(at, lane);
+    const uint8_t *at = mine ? walk.granule(0) : nullptr;
+    Granule<D> next = {};
+    if (at) next = load_granule<D>(at, lane);
+    for (uint32_t n = 0; n < mine; ++n) {
+        Granule<D> x = next;
+        const bool there = at != nullptr;
+        if (n + 1 < mine) {
+            if (((n + 1) & 63u) == 0) walk.refill(n + 1, mine - n - 1);
+            at = walk.granule(n + 1);
+            if (at) next = load_granule<D>(at, lane);
+        }
+        if (!there) continue;
+        const int32_t t0 = (int32_t)(32 * (from + skip + n * TOKEN_WAVES));
         // whether all rows see all of the granule
         const bool whole = t0 + 31 <= pos_first && (!a.window || (uint32_t)(pos_last - t0) < a.window);
+        const auto sees = [&](int i, int e) {
+            const int32_t t = t0 + 8 * (int32_t)g + e;
+            return t <= pos[i] && (!a.window || (uint32_t)(pos[i] - t) < a.window);
+        };
         if (!whole) {
             // tokens that no row sees may hold anything: their V scales become the least
             const int32_t t = t0 + 8 * (int32_t)g;
@@ -156,51 +189,59 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
             for (int e = 0; e < 8; ++e)
                 if (t + e > pos_last || t + e < low) x.vs[e / 4] &= ~(0xFFu << (8 * (e % 4)));
         }
-        // scores: half a, register e is token 8 g + 4 a + e
+        // scores: half h, register e is token 8 g + 4 h + e
         f32x4 sc[NR][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int i = 0; i < NR; ++i) sc[i][0] = sc[i][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < NR; ++i) sc[i][h] = f32x4{0, 0, 0, 0};
+        for (uint32_t j = 0; j < J; ++j) {
+            const Frag16 k0 = k_operand<T, D>(x, 0, (int)j), k1 = k_operand<T, D>(x, 1, (int)j);
 #pragma unroll
-            for (uint32_t j = 0; j < J; ++j) {
-                const Frag16 k = k_operand<T, D>(x, h, (int)j);
+            for (int i = 0; i < NR; ++i) {
+                Frag16 qi;
+                if constexpr (Q_LDS) qi.w = wave_q[(i * J + j) * 64];
+                else qi = q[i][j];
+                sc[i][0] = T == MMAEMU_BF16 ? mfma_bf16(k0, qi, sc[i][0]) : mfma_fp16(k0, qi, sc[i][0]);
+                sc[i][1] = T == MMAEMU_BF16 ? mfma_bf16(k1, qi, sc[i][1]) : mfma_fp16(k1, qi, sc[i][1]);
+            }
+        }
+        if (!whole) {
 #pragma unroll
-                for (int i = 0; i < NR; ++i) sc[i][h] = T == MMAEMU_BF16 ? mfma_bf16(k, q[i][j], sc[i][h]) : mfma_fp16(k, q[i][j], sc[i][h]);
+            for (int i = 0; i < NR; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sc[i][e / 4][e % 4] = sees(i, e) ? sc[i][e / 4][e % 4] : -__builtin_inff();
+        }
+        // The maximum moves where it falls behind by more than 2^LAG: weights stay below 2^(SHIFT + LAG), which FP16 holds.
+        float top[NR];
+        bool behind = false;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            float y = fmaxf(fmaxf(sc[i][0][0], sc[i][0][1]), sc[i][0][2]);
+            y = fmaxf(fmaxf(y, sc[i][0][3]), sc[i][1][0]);
+            y = fmaxf(fmaxf(y, sc[i][1][1]), sc[i][1][2]);
+            top[i] = other_rows_max(fmaxf(y, sc[i][1][3])) * a.c2;
+            behind = behind || top[i] > m[i] + LAG;
+        }
+        if (__any(behind)) {
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const float new_m = fmaxf(m[i], top[i]), factor = __builtin_amdgcn_exp2f(m[i] - new_m);
+                m[i] = new_m;
+                sum[i] *= factor;
+#pragma unroll
+                for (uint32_t d = 0; d < DT; ++d) acc[i][d] *= factor;
             }
         }
         Frag16 p[NR];
-        f16x8 seen[NR];
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            float top = LOWEST, z[8];
+            const float off = SHIFT - m[i];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                z[e] = sc[i][e / 4][e % 4] * a.c2;
-                if (!whole) {
-                    const int32_t t = t0 + 8 * (int32_t)g + e;
-                    const bool sees = t <= pos[i] && (!a.window || (uint32_t)(pos[i] - t) < a.window);
-                    z[e] = sees ? z[e] : -__builtin_inff();
-                    seen[i][e] = sees ? (_Float16)1.0f : (_Float16)0.0f;
-                } else seen[i][e] = (_Float16)1.0f;
-                top = fmaxf(top, z[e]);
+            for (int e = 0; e < 8; e += 2) {
+                const f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4], a.c2, off)),
+                                 __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4 + 1], a.c2, off))};
+                p[i].w[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
             }
-            top = fmaxf(m[i], other_rows_max(top));
-            const float factor = __builtin_amdgcn_exp2f(m[i] - top);
-            m[i] = top;
-            sum[i] *= factor;
-#pragma unroll
-            for (uint32_t d = 0; d < DT; ++d)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][d][e] *= factor;
-            f16x8 w;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float y = __builtin_amdgcn_exp2f(z[e] - top + SHIFT);
-                sum[i] += y;
-                w[e] = (_Float16)y;
-            }
-            p[i].w = __builtin_bit_cast(u32x4, w);
         }
         // NaN blocks among the values: they are taken as zeros, and make NaN the outputs of the rows that see them
         if (__any(any_nan_code(x.vs[0]) | any_nan_code(x.vs[1]))) {
@@ -213,24 +254,31 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
             }
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
-                const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad, seen[i], f32x4{0, 0, 0, 0}, 0, 0, 0);
+                f16x8 seen;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) seen[e] = sees(i, e) ? (_Float16)1.0f : (_Float16)0.0f;
+                const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad, seen, f32x4{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
                 for (uint32_t d = 0; d < DT; ++d)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i][d][e] = hit[e] > 0.0f ? __builtin_nanf("") : acc[i][d][e];
             }
         }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) sum[i] = mfma_fp16(ones, p[i], sum[i]);
         // values: word pairs of two elements 2 c, 2 c + 1 and eight tokens
+        float unit[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) unit[e] = __uint_as_float((x.vs[e / 4] >> (8 * (e % 4)) & 0xFFu) << 23);
 #pragma unroll
         for (uint32_t c = 0; c < DT / 2; ++c) {
             const uint32_t w0 = x.v[c / 2][2 * (c % 2)], w1 = x.v[c / 2][2 * (c % 2) + 1];
             f16x2 y[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float unit = __uint_as_float((x.vs[e / 4] >> (8 * (e % 4)) & 0xFFu) << 23);
                 const uint32_t w = e < 4 ? w0 : w1;
-                y[e] = e % 4 == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit, 0) : e % 4 == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit, 1) :
-                       e % 4 == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit, 2) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit, 3);
+                y[e] = e % 4 == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit[e], 0) : e % 4 == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit[e], 1) :
+                       e % 4 == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit[e], 2) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit[e], 3);
             }
             Frag16 even, odd;
 #pragma unroll
@@ -246,9 +294,6 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
             }
         }
     }
-
-#pragma unroll
-    for (int i = 0; i < NR; ++i) sum[i] = other_rows_sum(sum[i]);
 
     // one row's D / 16 outputs of register e, elements (4 g + e) D / 16 ..
     const auto store = [&](uint32_t r, uint32_t e, const float (&o)[DT], float rm, float rl) MMAEMU_INLINE {
@@ -285,13 +330,13 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
                 float o[DT];
 #pragma unroll
                 for (uint32_t d = 0; d < DT; ++d) o[d] = acc[i][d][e];
-                store(r0 + 16 * i + l, e, o, m[i], sum[i]);
+                store(r0 + 16 * i + l, e, o, m[i], sum[i][0]);
             }
     } else {
         // the wavefronts' parts of the same rows meet in LDS: rows are D + 4 numbers apart
 #pragma unroll
         for (int i = 0; i < NR; ++i)
-            if (g == 0) lds_stat[wave * 16 * NR + 16 * i + l] = f32x2{m[i], sum[i]};
+            if (g == 0) lds_stat[wave * 16 * NR + 16 * i + l] = f32x2{m[i], sum[i][0]};
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
@@ -372,7 +417,7 @@ static Plan plan_of(const mmaemu_attention_fp4_args &a)
 {
     const uint32_t rows = a.max_tokens * (a.heads / a.kv_heads);
     Plan p;
-    p.nr = rows <= 16 ? 1 : 2;
+    p.nr = rows <= 16 ? 1 : rows <= 64 ? 2 : 4;
     p.row_waves = rows <= 64 ? 1 : 4;
     p.block_rows = 16 * p.nr * p.row_waves;
     p.blocks = (rows + p.block_rows - 1) / p.block_rows;
@@ -396,7 +441,7 @@ uint64_t attention_fp4_workspace(const mmaemu_attention_fp4_args &a)
 template <int T, int D> static mmaemu_status launch_typed(const AttentionArgs &p, const Plan &plan, hipStream_t s)
 {
     const dim3 grid(plan.blocks * p.c.kv_heads, plan.splits, p.c.sequences);
-    if (plan.row_waves == 4) hipLaunchKernelGGL((attention_kernel<T, D, 2, 4>), grid, dim3(256), 0, s, p);
+    if (plan.row_waves == 4) hipLaunchKernelGGL((attention_kernel<T, D, 4, 4>), grid, dim3(256), 0, s, p);
     else if (plan.nr == 2) hipLaunchKernelGGL((attention_kernel<T, D, 2, 1>), grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL((attention_kernel<T, D, 1, 1>), grid, dim3(256), 0, s, p);
     MMAEMU_HIP(hipGetLastError());

@@ -23,7 +23,8 @@ struct AttentionArgs {
 };
 
 constexpr float LOWEST = -3.0e38f;                 // a maximum over nothing
-constexpr float SHIFT = 10.0f, LAG = 5.0f;         // weights are held times 2^SHIFT; how far (in log2) a maximum may fall behind
+constexpr float SHIFT = 10.0f;                     // weights are held times 2^SHIFT
+constexpr uint32_t LIMIT = 0x7800;                 // 2^15 in FP16: a weight that has come to this, 2^5 times its largest, moves the maximum
 
 // The granules that the rows r0 .. of a block see, and the part of them that a split takes.
 struct Range { uint32_t first, count, chunk; };
@@ -49,6 +50,14 @@ __device__ __forceinline__ float other_rows_max(float x)               // over l
     const uint32_t c = __float_as_uint(y);
     const auto q = __builtin_amdgcn_permlane16_swap(c, c, false, false);
     return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
+// the larger of each of two halves, as whole numbers (by hand: of a chain of the compiler's own, all but the first links were lost)
+__device__ __forceinline__ uint32_t packed_max(uint32_t x, uint32_t y)
+{
+    uint32_t z;
+    asm("v_pk_max_u16 %0, %1, %2" : "=v"(z) : "v"(x), "v"(y));
+    return z;
 }
 
 // a granule as a lane holds it
@@ -177,13 +186,16 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
         const int32_t t0 = (int32_t)(32 * (from + skip + n * TOKEN_WAVES));
         // whether all rows see all of the granule
         const bool whole = t0 + 31 <= pos_first && (!a.window || (uint32_t)(pos_last - t0) < a.window);
-        const auto sees = [&](int i, int e) {
-            const int32_t t = t0 + 8 * (int32_t)g + e;
-            return t <= pos[i] && (!a.window || (uint32_t)(pos[i] - t) < a.window);
+        const auto sees = [&](int32_t t, int i) { return t <= pos[i] && (!a.window || (uint32_t)(pos[i] - t) < a.window); };
+        // the lane's first token, for branches that few granules take: its value is hidden, or what is made of it would be made for all
+        const auto first_token = [&]() {
+            int32_t t = t0 + 8 * (int32_t)g;
+            asm volatile("" : "+v"(t));
+            return t;
         };
         if (!whole) {
             // tokens that no row sees may hold anything: their V scales become the least
-            const int32_t t = t0 + 8 * (int32_t)g;
+            const int32_t t = first_token();
             const int32_t low = a.window && (uint32_t)(pos_first < 0 ? 0 : pos_first) >= a.window ? pos_first + 1 - (int32_t)a.window : 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -206,45 +218,48 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
             }
         }
         if (!whole) {
+            const int32_t t = first_token();
 #pragma unroll
             for (int i = 0; i < NR; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sc[i][e / 4][e % 4] = sees(i, e) ? sc[i][e / 4][e % 4] : -__builtin_inff();
+                for (int e = 0; e < 8; ++e) sc[i][e / 4][e % 4] = sees(t + e, i) ? sc[i][e / 4][e % 4] : -__builtin_inff();
         }
-        // The maximum moves where it falls behind by more than 2^LAG: weights stay below 2^(SHIFT + LAG), which FP16 holds.
-        float top[NR];
-        bool behind = false;
-#pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            float y = fmaxf(fmaxf(sc[i][0][0], sc[i][0][1]), sc[i][0][2]);
-            y = fmaxf(fmaxf(y, sc[i][0][3]), sc[i][1][0]);
-            y = fmaxf(fmaxf(y, sc[i][1][1]), sc[i][1][2]);
-            top[i] = other_rows_max(fmaxf(y, sc[i][1][3])) * a.c2;
-            behind = behind || top[i] > m[i] + LAG;
-        }
-        if (__any(behind)) {
+        // Weights against the maximum as it was.  Where one comes to LIMIT or more (or is NaN), the maximum moves and they are made again: below
+        // that FP16 holds them, and their patterns' order as integers is theirs.
+        Frag16 p[NR];
+        const auto weights = [&]() MMAEMU_INLINE {
+            uint32_t most = 0;
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
-                const float new_m = fmaxf(m[i], top[i]), factor = __builtin_amdgcn_exp2f(m[i] - new_m);
-                m[i] = new_m;
+                const float off = SHIFT - m[i];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4], a.c2, off)),
+                                     __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4 + 1], a.c2, off))};
+                    p[i].w[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
+                    most = packed_max(most, p[i].w[e / 2]);
+                }
+            }
+            return most;
+        };
+        const uint32_t most = weights();
+        if (__any((most + (0x8000u - LIMIT) * 0x10001u & 0x80008000u) != 0)) {
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                float top = fmaxf(fmaxf(sc[i][0][0], sc[i][0][1]), fmaxf(sc[i][0][2], sc[i][0][3]));
+                top = fmaxf(top, fmaxf(fmaxf(sc[i][1][0], sc[i][1][1]), fmaxf(sc[i][1][2], sc[i][1][3])));
+                top = fmaxf(m[i], other_rows_max(top) * a.c2);
+                const float factor = __builtin_amdgcn_exp2f(m[i] - top);
+                m[i] = top;
                 sum[i] *= factor;
 #pragma unroll
                 for (uint32_t d = 0; d < DT; ++d) acc[i][d] *= factor;
             }
-        }
-        Frag16 p[NR];
-#pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            const float off = SHIFT - m[i];
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4], a.c2, off)),
-                                 __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4 + 1], a.c2, off))};
-                p[i].w[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
-            }
+            weights();
         }
         // NaN blocks among the values: they are taken as zeros, and make NaN the outputs of the rows that see them
         if (__any(any_nan_code(x.vs[0]) | any_nan_code(x.vs[1]))) {
+            const int32_t t = first_token();
             f16x8 bad;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -256,7 +271,7 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
             for (int i = 0; i < NR; ++i) {
                 f16x8 seen;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) seen[e] = sees(i, e) ? (_Float16)1.0f : (_Float16)0.0f;
+                for (int e = 0; e < 8; ++e) seen[e] = sees(t + e, i) ? (_Float16)1.0f : (_Float16)0.0f;
                 const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad, seen, f32x4{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
                 for (uint32_t d = 0; d < DT; ++d)

@@ -60,34 +60,29 @@ __device__ __forceinline__ uint32_t packed_max(uint32_t x, uint32_t y)
     return z;
 }
 
-// a granule as a lane holds it
-template <int D> struct Granule {
-    u32x4 k[D / 64], v[D / 64];
-    uint32_t ks;                                   // its K scales of both halves
-    uint32_t vs[2];                                // its V scales of eight tokens
-};
-template <int D> __device__ __forceinline__ Granule<D> load_granule(const uint8_t *at, uint32_t lane)
+// a granule as a lane holds it: keys with the scales of both halves, values with the scales of eight tokens
+template <int D> struct Keys { u32x4 k[D / 64]; uint32_t scales; };
+template <int D> struct Values { u32x4 v[D / 64]; uint32_t scales[2]; };
+template <int D> __device__ __forceinline__ void load_keys(Keys<D> &x, const uint8_t *at, uint32_t lane)
 {
-    const uint32_t g = lane >> 4, l = lane & 15u;
-    constexpr uint32_t B = D / 32;
-    Granule<D> x;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-        x.k[i] = *reinterpret_cast<const u32x4 *>(at + 1024 * i + 16 * lane);
-        x.v[i] = *reinterpret_cast<const u32x4 *>(at + 16 * D + 1024 * i + 16 * lane);
-    }
-    x.ks = *reinterpret_cast<const uint16_t *>(at + 32 * D + (g * B / 4 * 16 + l) * 2);
-    const uint32_t *vs = reinterpret_cast<const uint32_t *>(at + 33 * D + (g * B + l * B / 16) * 8);
-    x.vs[0] = vs[0];
-    x.vs[1] = vs[1];
-    return x;
+    for (int i = 0; i < D / 64; ++i) x.k[i] = *reinterpret_cast<const u32x4 *>(at + 1024 * i + 16 * lane);
+    x.scales = *reinterpret_cast<const uint16_t *>(at + 32 * D + ((lane >> 4) * (D / 32) / 4 * 16 + (lane & 15u)) * 2);
+}
+template <int D> __device__ __forceinline__ void load_values(Values<D> &x, const uint8_t *at, uint32_t lane)
+{
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) x.v[i] = *reinterpret_cast<const u32x4 *>(at + 16 * D + 1024 * i + 16 * lane);
+    const Words2<8> w = *reinterpret_cast<const Words2<8> *>(at + 33 * D + ((lane >> 4) * (D / 32) + (lane & 15u) * (D / 32) / 16) * 8);
+    x.scales[0] = w.w[0];
+    x.scales[1] = w.w[1];
 }
 
-// the 16-bit K operand of half a, dimensions 8 j .. 8 j + 7 of the lane's D / 4
-template <int T, int D> __device__ __forceinline__ Frag16 k_operand(const Granule<D> &x, int a, int j)
+// the 16-bit K operand of half a, elements 8 j .. 8 j + 7 of the lane's D / 4
+template <int T, int D> __device__ __forceinline__ Frag16 k_operand(const Keys<D> &x, int a, int j)
 {
     const uint32_t word = D == 128 ? x.k[D == 128 ? a : 0][j] : x.k[0][2 * a + j];
-    const uint32_t code = a ? x.ks >> 8 : x.ks & 0xFFu;
+    const uint32_t code = a ? x.scales >> 8 : x.scales & 0xFFu;
     return T == MMAEMU_BF16 ? weights_bf16(word, code) : weights_fp16(word, code);
 }
 
@@ -171,18 +166,29 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
         for (uint32_t d = 0; d < DT; ++d) acc[i][d] = f32x4{0, 0, 0, 0};
     }
 
-    const uint8_t *at = mine ? walk.granule(0) : nullptr;
-    Granule<D> next = {};
-    if (at) next = load_granule<D>(at, lane);
+    // The next granule's keys are read once this one's are used, its values once this one's are: they stay on their way during the other's products.
+    // (Where there is no next one, or its page is none, the first granule of the memory is read: a load that always happens costs no branch.)
+    bool there = false;
+    const uint8_t *at = walk.base;
+    const auto advance = [&](uint32_t n) MMAEMU_INLINE {
+        const uint8_t *const next = n < mine ? walk.granule(n) : nullptr;
+        there = next != nullptr;
+        at = there ? next : walk.base;
+    };
+    advance(0);
+    Keys<D> xk;
+    Values<D> xv;
+    load_keys<D>(xk, at, lane);
+    load_values<D>(xv, at, lane);
     for (uint32_t n = 0; n < mine; ++n) {
-        Granule<D> x = next;
-        const bool there = at != nullptr;
-        if (n + 1 < mine) {
-            if (((n + 1) & 63u) == 0) walk.refill(n + 1, mine - n - 1);
-            at = walk.granule(n + 1);
-            if (at) next = load_granule<D>(at, lane);
+        const bool now = there;
+        if (((n + 1) & 63u) == 0 && n + 1 < mine) walk.refill(n + 1, mine - n - 1);
+        advance(n + 1);
+        if (!now) {
+            load_keys<D>(xk, at, lane);
+            load_values<D>(xv, at, lane);
+            continue;
         }
-        if (!there) continue;
         const int32_t t0 = (int32_t)(32 * (from + skip + n * TOKEN_WAVES));
         // whether all rows see all of the granule
         const bool whole = t0 + 31 <= pos_first && (!a.window || (uint32_t)(pos_last - t0) < a.window);
@@ -199,7 +205,7 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
             const int32_t low = a.window && (uint32_t)(pos_first < 0 ? 0 : pos_first) >= a.window ? pos_first + 1 - (int32_t)a.window : 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (t + e > pos_last || t + e < low) x.vs[e / 4] &= ~(0xFFu << (8 * (e % 4)));
+                if (t + e > pos_last || t + e < low) xv.scales[e / 4] &= ~(0xFFu << (8 * (e % 4)));
         }
         // scores: half h, register e is token 8 g + 4 h + e
         f32x4 sc[NR][2];
@@ -207,7 +213,7 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
         for (int i = 0; i < NR; ++i) sc[i][0] = sc[i][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (uint32_t j = 0; j < J; ++j) {
-            const Frag16 k0 = k_operand<T, D>(x, 0, (int)j), k1 = k_operand<T, D>(x, 1, (int)j);
+            const Frag16 k0 = k_operand<T, D>(xk, 0, (int)j), k1 = k_operand<T, D>(xk, 1, (int)j);
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
                 Frag16 qi;
@@ -217,6 +223,7 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
                 sc[i][1] = T == MMAEMU_BF16 ? mfma_bf16(k1, qi, sc[i][1]) : mfma_fp16(k1, qi, sc[i][1]);
             }
         }
+        load_keys<D>(xk, at, lane);
         if (!whole) {
             const int32_t t = first_token();
 #pragma unroll
@@ -224,28 +231,25 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sc[i][e / 4][e % 4] = sees(t + e, i) ? sc[i][e / 4][e % 4] : -__builtin_inff();
         }
-        // Weights against the maximum as it was.  Where one comes to LIMIT or more (or is NaN), the maximum moves and they are made again: below
+        // Weights against the maximum as it was.  Where one of a tile comes to LIMIT or more (or is NaN), its maxima move and its weights are made again: below
         // that FP16 holds them, and their patterns' order as integers is theirs.
         Frag16 p[NR];
-        const auto weights = [&]() MMAEMU_INLINE {
+        const auto weights = [&](int i) MMAEMU_INLINE {
             uint32_t most = 0;
+            const float off = SHIFT - m[i];
 #pragma unroll
-            for (int i = 0; i < NR; ++i) {
-                const float off = SHIFT - m[i];
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4], a.c2, off)),
-                                     __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4 + 1], a.c2, off))};
-                    p[i].w[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
-                    most = packed_max(most, p[i].w[e / 2]);
-                }
+            for (int e = 0; e < 8; e += 2) {
+                const f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4], a.c2, off)),
+                                 __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4 + 1], a.c2, off))};
+                p[i].w[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
+                most = e ? packed_max(most, p[i].w[e / 2]) : p[i].w[0];
             }
             return most;
         };
-        const uint32_t most = weights();
-        if (__any((most + (0x8000u - LIMIT) * 0x10001u & 0x80008000u) != 0)) {
 #pragma unroll
-            for (int i = 0; i < NR; ++i) {
+        for (int i = 0; i < NR; ++i) {
+            const uint32_t most = weights(i);
+            if (__any((most + (0x8000u - LIMIT) * 0x10001u & 0x80008000u) != 0)) {
                 float top = fmaxf(fmaxf(sc[i][0][0], sc[i][0][1]), fmaxf(sc[i][0][2], sc[i][0][3]));
                 top = fmaxf(top, fmaxf(fmaxf(sc[i][1][0], sc[i][1][1]), fmaxf(sc[i][1][2], sc[i][1][3])));
                 top = fmaxf(m[i], other_rows_max(top) * a.c2);
@@ -254,18 +258,18 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
                 sum[i] *= factor;
 #pragma unroll
                 for (uint32_t d = 0; d < DT; ++d) acc[i][d] *= factor;
+                weights(i);
             }
-            weights();
         }
         // NaN blocks among the values: they are taken as zeros, and make NaN the outputs of the rows that see them
-        if (__any(any_nan_code(x.vs[0]) | any_nan_code(x.vs[1]))) {
+        if (__any(any_nan_code(xv.scales[0]) | any_nan_code(xv.scales[1]))) {
             const int32_t t = first_token();
             f16x8 bad;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const bool nan = (x.vs[e / 4] >> (8 * (e % 4)) & 0xFFu) == 0xFFu;
+                const bool nan = (xv.scales[e / 4] >> (8 * (e % 4)) & 0xFFu) == 0xFFu;
                 bad[e] = nan ? (_Float16)1.0f : (_Float16)0.0f;
-                if (nan) x.vs[e / 4] &= ~(0xFFu << (8 * (e % 4)));
+                if (nan) xv.scales[e / 4] &= ~(0xFFu << (8 * (e % 4)));
             }
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
@@ -284,10 +288,10 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
         // values: word pairs of two elements 2 c, 2 c + 1 and eight tokens
         float unit[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) unit[e] = __uint_as_float((x.vs[e / 4] >> (8 * (e % 4)) & 0xFFu) << 23);
+        for (int e = 0; e < 8; ++e) unit[e] = __uint_as_float((xv.scales[e / 4] >> (8 * (e % 4)) & 0xFFu) << 23);
 #pragma unroll
         for (uint32_t c = 0; c < DT / 2; ++c) {
-            const uint32_t w0 = x.v[c / 2][2 * (c % 2)], w1 = x.v[c / 2][2 * (c % 2) + 1];
+            const uint32_t w0 = xv.v[c / 2][2 * (c % 2)], w1 = xv.v[c / 2][2 * (c % 2) + 1];
             f16x2 y[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -308,6 +312,7 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
                 acc[i][2 * c + 1] = mfma_fp16(odd, p[i], acc[i][2 * c + 1]);
             }
         }
+        load_values<D>(xv, at, lane);
     }
 
     // one row's D / 16 outputs of register e, elements (4 g + e) D / 16 ..

@@ -4,8 +4,7 @@
 // over the tokens with a running maximum m and sum l per row, in units of log2:
 //   s = scale log2(e) q.k;  m' = max(m, max s);  p = 2^(s - m');  l = l 2^(m - m') + sum p;  O = O 2^(m - m') + p V;  out = O / l
 // Both products are 16 x 16 x 32 instructions on operands that lie in the cache as the lanes take them (cache_fp4.hpp), brought to 16 bits, which is
-// exact: K to the queries' type, V to FP16.  The scores' registers are the second product's operand as they are, rounded to FP16 after a shift by 2^10:
-// weights down to 2^-24 of the largest keep all their bits.
+// exact: K to the queries' type, V to FP16.  The scores' registers are the second product's operand as they are, rounded to FP16.
 #include "cache_fp4.hpp"
 #include "fp4_operands.hpp"
 
@@ -18,17 +17,19 @@ struct AttentionArgs {
     float *part;                                   // [split][token][head][D], unnormalised, and behind them
     f32x2 *stat;                                   // [split][token][head] (m, l)
     uint64_t q_stride, out_stride;
-    uint32_t heads, group, max_tokens, window, splits, blocks;         // blocks: of rows, of a sequence's KV head
+    uint32_t heads, group, max_tokens, window, blocks;                 // blocks: of rows, of a sequence's KV head
+    uint32_t splits, chunk;                        // most workgroups that share a row's granules, and how many granules make one more worth it
     float c2;                                      // scale log2(e)
 };
 
 constexpr float LOWEST = -3.0e38f;                 // a maximum over nothing
-constexpr float SHIFT = 10.0f;                     // weights are held times 2^SHIFT
-constexpr uint32_t LIMIT = 0x7800;                 // 2^15 in FP16: a weight that has come to this, 2^5 times its largest, moves the maximum
+// Weights are held times 2^SHIFT, relative to a maximum that moves where those of a granule come to LIMIT together: it may lie 2^11 below.  Weights down to 2^-18
+// of the largest keep FP16's eleven bits, and smaller ones are off by 2^-29 of it at most.
+constexpr float SHIFT = 4.0f, LIMIT = 32768.0f;
 
-// The granules that the rows r0 .. of a block see, and the part of them that a split takes.
-struct Range { uint32_t first, count, chunk; };
-__device__ __forceinline__ Range granules_of(const AttentionArgs &a, const Sequence &sq, uint32_t r0, uint32_t rows, uint32_t least)
+// The granules that the rows r0 .. of a block see, and the parts that workgroups take of them, `chunk` each.
+struct Range { uint32_t first, count, parts, chunk; };
+__device__ __forceinline__ Range granules_of(const AttentionArgs &a, const Sequence &sq, uint32_t r0, uint32_t rows)
 {
     const uint32_t all = (sq.n < a.max_tokens ? sq.n : a.max_tokens) * a.group;
     const uint32_t last = (r0 + rows < all ? r0 + rows : all) - 1;
@@ -37,8 +38,13 @@ __device__ __forceinline__ Range granules_of(const AttentionArgs &a, const Seque
     Range g;
     g.first = (uint32_t)begin / 32u;
     g.count = end > begin ? ((uint32_t)end + 31u) / 32u - g.first : 0u;
-    const uint32_t even = (g.count + a.splits - 1) / a.splits;
-    g.chunk = even > least ? even : least;
+    g.parts = 1;
+    g.chunk = g.count;
+    if (a.splits > 1) {
+        g.parts = (g.count + a.chunk - 1) / a.chunk;
+        g.parts = g.parts < 1 ? 1u : g.parts > a.splits ? a.splits : g.parts;
+        g.chunk = (g.count + g.parts - 1) / g.parts;
+    }
     return g;
 }
 
@@ -52,38 +58,73 @@ __device__ __forceinline__ float other_rows_max(float x)               // over l
     return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
 }
 
-// the larger of each of two halves, as whole numbers (by hand: of a chain of the compiler's own, all but the first links were lost)
-__device__ __forceinline__ uint32_t packed_max(uint32_t x, uint32_t y)
-{
-    uint32_t z;
-    asm("v_pk_max_u16 %0, %1, %2" : "=v"(z) : "v"(x), "v"(y));
-    return z;
-}
-
 // a granule as a lane holds it: keys with the scales of both halves, values with the scales of eight tokens
 template <int D> struct Keys { u32x4 k[D / 64]; uint32_t scales; };
 template <int D> struct Values { u32x4 v[D / 64]; uint32_t scales[2]; };
-template <int D> __device__ __forceinline__ void load_keys(Keys<D> &x, const uint8_t *at, uint32_t lane)
+// A lane's places in a granule.  Their values are hidden, so that a load adds them to the granule's uniform address by itself.
+template <int D> struct Offsets {
+    uint32_t codes, key_scales, value_scales;
+    __device__ __forceinline__ explicit Offsets(uint32_t lane)
+    {
+        constexpr uint32_t B = D / 32;
+        codes = 16 * lane;
+        key_scales = 32 * D + ((lane >> 4) * B / 4 * 16 + (lane & 15u)) * 2;
+        value_scales = 33 * D + ((lane >> 4) * B + (lane & 15u) * B / 16) * 8;
+        asm volatile("" : "+v"(codes), "+v"(key_scales), "+v"(value_scales));
+    }
+};
+template <int D> __device__ __forceinline__ void load_keys(Keys<D> &x, const uint8_t *at, const Offsets<D> &off)
 {
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) x.k[i] = *reinterpret_cast<const u32x4 *>(at + 1024 * i + 16 * lane);
-    x.scales = *reinterpret_cast<const uint16_t *>(at + 32 * D + ((lane >> 4) * (D / 32) / 4 * 16 + (lane & 15u)) * 2);
+    for (int i = 0; i < D / 64; ++i) x.k[i] = *reinterpret_cast<const u32x4 *>(at + 1024 * i + off.codes);
+    x.scales = *reinterpret_cast<const uint16_t *>(at + off.key_scales);
 }
-template <int D> __device__ __forceinline__ void load_values(Values<D> &x, const uint8_t *at, uint32_t lane)
+template <int D> __device__ __forceinline__ void load_values(Values<D> &x, const uint8_t *at, const Offsets<D> &off)
 {
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) x.v[i] = *reinterpret_cast<const u32x4 *>(at + 16 * D + 1024 * i + 16 * lane);
-    const Words2<8> w = *reinterpret_cast<const Words2<8> *>(at + 33 * D + ((lane >> 4) * (D / 32) + (lane & 15u) * (D / 32) / 16) * 8);
+    for (int i = 0; i < D / 64; ++i) x.v[i] = *reinterpret_cast<const u32x4 *>(at + 16 * D + 1024 * i + off.codes);
+    const Words2<8> w = *reinterpret_cast<const Words2<8> *>(at + off.value_scales);
     x.scales[0] = w.w[0];
     x.scales[1] = w.w[1];
 }
 
-// the 16-bit K operand of half a, elements 8 j .. 8 j + 7 of the lane's D / 4
-template <int T, int D> __device__ __forceinline__ Frag16 k_operand(const Keys<D> &x, int a, int j)
+// The conversions read the exponent field of their scale alone (all 256 fields with other bits around them: no difference), so a code needs no more than
+// to be shifted there.
+template <int BYTE> __device__ __forceinline__ float scale_of(uint32_t codes)
 {
-    const uint32_t word = D == 128 ? x.k[D == 128 ? a : 0][j] : x.k[0][2 * a + j];
-    const uint32_t code = a ? x.scales >> 8 : x.scales & 0xFFu;
-    return T == MMAEMU_BF16 ? weights_bf16(word, code) : weights_fp16(word, code);
+    return __uint_as_float(BYTE == 0 ? codes << 23 : BYTE == 1 ? codes << 15 : BYTE == 2 ? codes << 7 : codes >> 1);
+}
+__device__ __forceinline__ Frag16 keys_bf16(uint32_t codes, float s)
+{
+    Frag16 f;
+    f.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0));
+    f.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1));
+    f.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2));
+    f.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3));
+    return f;
+}
+__device__ __forceinline__ Frag16 keys_fp16(uint32_t codes, float s)
+{
+    Frag16 f;
+    f.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 0));
+    f.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 1));
+    f.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 2));
+    f.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 3));
+    return f;
+}
+// the 16-bit K operand of half A, elements 8 j .. 8 j + 7 of the lane's D / 4
+template <int T, int D, int A> __device__ __forceinline__ Frag16 k_operand(const Keys<D> &x, int j)
+{
+    const uint32_t word = D == 128 ? x.k[D == 128 ? A : 0][j] : x.k[0][2 * A + j];
+    return T == MMAEMU_BF16 ? keys_bf16(word, scale_of<A>(x.scales)) : keys_fp16(word, scale_of<A>(x.scales));
+}
+// two elements of tokens 4 H .. 4 H + 3, a byte each, under those tokens' scales
+template <int H> __device__ __forceinline__ void four_values(uint32_t word, const uint32_t (&scales)[2], f16x2 (&y)[8])
+{
+    y[4 * H] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_of<0>(scales[H]), 0);
+    y[4 * H + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_of<1>(scales[H]), 1);
+    y[4 * H + 2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_of<2>(scales[H]), 2);
+    y[4 * H + 3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_of<3>(scales[H]), 3);
 }
 
 // codes of bytes 0xFF in a word, as 0x80 in their bytes (exact: the lowest byte that is one is found, and those above it)
@@ -109,25 +150,26 @@ template <int D> struct Walk {
     }
 };
 
-// Rows of NR x 16 x ROW_WAVES, tokens split over the other wavefronts of four.  Where the tiles of rows are many, the queries wait in LDS.
-template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__(256, NR == 1 ? 3 : 2) attention_kernel(const AttentionArgs a)
+// Rows of NR x 16 x ROW_WAVES, tokens split over the other wavefronts.  Where the tiles of rows are many, the queries wait in LDS.
+template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __launch_bounds__(64 * WAVES, NR == 1 ? 4 : D == 64 ? (NR == 2 ? 4 : NR == 3 ? 3 : 2) : 2) attention_kernel(const AttentionArgs a)
 {
-    constexpr uint32_t WAVES = 4, TOKEN_WAVES = WAVES / ROW_WAVES, J = D / 32, DT = D / 16;
+    constexpr uint32_t TOKEN_WAVES = WAVES / ROW_WAVES, J = D / 32, DT = D / 16;
     constexpr uint32_t ROWS = 16 * NR * ROW_WAVES;
     constexpr bool Q_LDS = NR >= 4;
-    __shared__ __attribute__((aligned(16))) float lds[TOKEN_WAVES > 1 ? TOKEN_WAVES * 16 * NR * (D + 4) : 1];
+    __shared__ __attribute__((aligned(16))) float lds[TOKEN_WAVES > 1 ? TOKEN_WAVES * 16 * (D + 4) : 1];
     __shared__ f32x2 lds_stat[TOKEN_WAVES > 1 ? TOKEN_WAVES * 16 * NR : 1];
-    __shared__ u32x4 lds_q[Q_LDS ? WAVES * NR * J * 64 : 1];
+    __shared__ u32x4 lds_q[Q_LDS ? ROW_WAVES * NR * J * 64 : 1];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15u;
     const uint32_t head = blockIdx.x % a.c.kv_heads, block = a.blocks - 1 - blockIdx.x / a.c.kv_heads;        // the longest rows first
     const uint32_t split = blockIdx.y, s = blockIdx.z;
     const Sequence sq = sequence_of(a.c, s);
     const uint32_t rows = (sq.n < a.max_tokens ? sq.n : a.max_tokens) * a.group;
     if (block * ROWS >= rows) return;
-    const Range range = granules_of(a, sq, block * ROWS, ROWS, 2 * TOKEN_WAVES);
+    const Range range = granules_of(a, sq, block * ROWS, ROWS);
+    if (split >= range.parts) return;
     const uint32_t begin = split * range.chunk;
-    if (a.splits > 1 && begin >= range.count) return;
     uint32_t count = range.count > begin ? (range.count - begin < range.chunk ? range.count - begin : range.chunk) : 0u;
+    const bool direct = range.parts == 1;
     const uint32_t r0 = block * ROWS + (ROW_WAVES > 1 ? wave * 16 * NR : 0);
     // positions of the wavefront's first and last rows; its granules
     const uint32_t r_last = (r0 + 16 * NR < rows ? r0 + 16 * NR : rows) - 1;
@@ -140,53 +182,58 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
 
     // this lane's rows: query operands, and positions (rows that are not there: the last one again)
     Frag16 q[Q_LDS ? 1 : NR][J];
-    u32x4 *const wave_q = lds_q + wave * (NR * J * 64) + lane;
+    u32x4 *const wave_q = lds_q + (ROW_WAVES > 1 ? wave * (NR * J * 64) : 0) + lane;
     int32_t pos[NR];
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const uint32_t r = r0 + 16 * i + l < rows ? r0 + 16 * i + l : rows - 1, token = r / a.group, h = r % a.group;
         pos[i] = sq.start + (int32_t)token;
+        if (Q_LDS && ROW_WAVES == 1 && (uint32_t)i % WAVES != wave) continue;      // (the same for all wavefronts: they share them)
         const uint16_t *at = (const uint16_t *)a.q + (uint64_t)(sq.first + token) * a.q_stride + (uint64_t)(head * a.group + h) * D + g * (D / 4);
 #pragma unroll
         for (uint32_t j = 0; j < J; ++j) {
             const u32x4 w = *reinterpret_cast<const u32x4 *>(at + 8 * j);
-            if constexpr (Q_LDS) wave_q[(i * J + j) * 64] = w;         // (read by the lane that wrote it)
+            if constexpr (Q_LDS) wave_q[(i * J + j) * 64] = w;
             else q[i][j].w = w;
         }
     }
 
+    if (Q_LDS && ROW_WAVES == 1) __syncthreads();
+
     const Frag16 ones = {{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u}};
     float m[NR];
-    f32x4 acc[NR][DT], sum[NR];                    // (a sum is in all four)
+    f32x4 acc[NR][DT];
+    float sum[NR];
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         m[i] = LOWEST;
-        sum[i] = f32x4{0, 0, 0, 0};
+        sum[i] = 0.0f;
 #pragma unroll
         for (uint32_t d = 0; d < DT; ++d) acc[i][d] = f32x4{0, 0, 0, 0};
     }
 
-    // The next granule's keys are read once this one's are used, its values once this one's are: they stay on their way during the other's products.
-    // (Where there is no next one, or its page is none, the first granule of the memory is read: a load that always happens costs no branch.)
+    // The next granule's keys are read once this one's are used, its values once this one's are: they are on their way during the other's products.
+    // (Where a page is none, and past the end, the first granule of the memory is read: a load that always happens costs no branch.)
     bool there = false;
     const uint8_t *at = walk.base;
     const auto advance = [&](uint32_t n) MMAEMU_INLINE {
+        if ((n & 63u) == 0 && n && n < mine) walk.refill(n, mine - n);
         const uint8_t *const next = n < mine ? walk.granule(n) : nullptr;
         there = next != nullptr;
         at = there ? next : walk.base;
     };
-    advance(0);
+    const Offsets<D> off(lane);
     Keys<D> xk;
     Values<D> xv;
-    load_keys<D>(xk, at, lane);
-    load_values<D>(xv, at, lane);
+    advance(0);
+    load_keys<D>(xk, at, off);
+    load_values<D>(xv, at, off);
     for (uint32_t n = 0; n < mine; ++n) {
         const bool now = there;
-        if (((n + 1) & 63u) == 0 && n + 1 < mine) walk.refill(n + 1, mine - n - 1);
         advance(n + 1);
         if (!now) {
-            load_keys<D>(xk, at, lane);
-            load_values<D>(xv, at, lane);
+            load_keys<D>(xk, at, off);
+            load_values<D>(xv, at, off);
             continue;
         }
         const int32_t t0 = (int32_t)(32 * (from + skip + n * TOKEN_WAVES));
@@ -213,7 +260,7 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
         for (int i = 0; i < NR; ++i) sc[i][0] = sc[i][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (uint32_t j = 0; j < J; ++j) {
-            const Frag16 k0 = k_operand<T, D>(xk, 0, (int)j), k1 = k_operand<T, D>(xk, 1, (int)j);
+            const Frag16 k0 = k_operand<T, D, 0>(xk, (int)j), k1 = k_operand<T, D, 1>(xk, (int)j);
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
                 Frag16 qi;
@@ -223,7 +270,7 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
                 sc[i][1] = T == MMAEMU_BF16 ? mfma_bf16(k1, qi, sc[i][1]) : mfma_fp16(k1, qi, sc[i][1]);
             }
         }
-        load_keys<D>(xk, at, lane);
+        load_keys<D>(xk, at, off);
         if (!whole) {
             const int32_t t = first_token();
 #pragma unroll
@@ -231,25 +278,33 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sc[i][e / 4][e % 4] = sees(t + e, i) ? sc[i][e / 4][e % 4] : -__builtin_inff();
         }
-        // Weights against the maximum as it was.  Where one of a tile comes to LIMIT or more (or is NaN), its maxima move and its weights are made again: below
-        // that FP16 holds them, and their patterns' order as integers is theirs.
+        // Weights against the maximum as it was, and their sums over the granule, which the matrix instruction makes as well.  Where a sum comes to LIMIT (or is
+        // NaN, or a weight has left FP16), the maxima move and the weights are made again.
         Frag16 p[NR];
-        const auto weights = [&](int i) MMAEMU_INLINE {
-            uint32_t most = 0;
-            const float off = SHIFT - m[i];
+        float add[NR];
+        for (bool moved = false;; moved = true) {
+            f32x4 total[NR];
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4], a.c2, off)),
-                                 __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4 + 1], a.c2, off))};
-                p[i].w[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
-                most = e ? packed_max(most, p[i].w[e / 2]) : p[i].w[0];
+            for (int i = 0; i < NR; ++i) {
+                const float off = SHIFT - m[i];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4], a.c2, off)),
+                                     __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4 + 1], a.c2, off))};
+                    p[i].w[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
+                }
+                total[i] = mfma_fp16(ones, p[i], f32x4{0, 0, 0, 0});
             }
-            return most;
-        };
+            bool over = false;
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            const uint32_t most = weights(i);
-            if (__any((most + (0x8000u - LIMIT) * 0x10001u & 0x80008000u) != 0)) {
+            for (int i = 0; i < NR; ++i) {
+                add[i] = total[i][0];
+                over = over || !(add[i] < LIMIT);
+            }
+            if (moved || !__any(over)) break;
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                if (!__any(!(add[i] < LIMIT))) continue;
                 float top = fmaxf(fmaxf(sc[i][0][0], sc[i][0][1]), fmaxf(sc[i][0][2], sc[i][0][3]));
                 top = fmaxf(top, fmaxf(fmaxf(sc[i][1][0], sc[i][1][1]), fmaxf(sc[i][1][2], sc[i][1][3])));
                 top = fmaxf(m[i], other_rows_max(top) * a.c2);
@@ -258,9 +313,10 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
                 sum[i] *= factor;
 #pragma unroll
                 for (uint32_t d = 0; d < DT; ++d) acc[i][d] *= factor;
-                weights(i);
             }
         }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) sum[i] += add[i];
         // NaN blocks among the values: they are taken as zeros, and make NaN the outputs of the rows that see them
         if (__any(any_nan_code(xv.scales[0]) | any_nan_code(xv.scales[1]))) {
             const int32_t t = first_token();
@@ -283,22 +339,12 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
                     for (int e = 0; e < 4; ++e) acc[i][d][e] = hit[e] > 0.0f ? __builtin_nanf("") : acc[i][d][e];
             }
         }
-#pragma unroll
-        for (int i = 0; i < NR; ++i) sum[i] = mfma_fp16(ones, p[i], sum[i]);
         // values: word pairs of two elements 2 c, 2 c + 1 and eight tokens
-        float unit[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) unit[e] = __uint_as_float((xv.scales[e / 4] >> (8 * (e % 4)) & 0xFFu) << 23);
 #pragma unroll
         for (uint32_t c = 0; c < DT / 2; ++c) {
-            const uint32_t w0 = xv.v[c / 2][2 * (c % 2)], w1 = xv.v[c / 2][2 * (c % 2) + 1];
             f16x2 y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t w = e < 4 ? w0 : w1;
-                y[e] = e % 4 == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit[e], 0) : e % 4 == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit[e], 1) :
-                       e % 4 == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit[e], 2) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit[e], 3);
-            }
+            four_values<0>(xv.v[c / 2][2 * (c % 2)], xv.scales, y);
+            four_values<1>(xv.v[c / 2][2 * (c % 2) + 1], xv.scales, y);
             Frag16 even, odd;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -312,142 +358,158 @@ template <int T, int D, int NR, int ROW_WAVES> __global__ void __launch_bounds__
                 acc[i][2 * c + 1] = mfma_fp16(odd, p[i], acc[i][2 * c + 1]);
             }
         }
-        load_values<D>(xv, at, lane);
+        load_values<D>(xv, at, off);
     }
 
-    // one row's D / 16 outputs of register e, elements (4 g + e) D / 16 ..
-    const auto store = [&](uint32_t r, uint32_t e, const float (&o)[DT], float rm, float rl) MMAEMU_INLINE {
-        if (r >= rows) return;
-        const uint64_t token = sq.first + r / a.group;
-        const uint32_t h = head * a.group + r % a.group, at = (4 * g + e) * DT;
-        if (a.splits > 1) {
-            const uint64_t row = ((uint64_t)split * a.c.tokens + token) * a.heads + h;
-            float *to = a.part + row * D + at;
-#pragma unroll
-            for (uint32_t d = 0; d < DT; d += 4) *reinterpret_cast<f32x4 *>(to + d) = f32x4{o[d], o[d + 1], o[d + 2], o[d + 3]};
-            if (e == 0 && g == 0) a.stat[row] = f32x2{rm, rl};
-            return;
-        }
-        const float inverse = rl == 0.0f ? 0.0f : 1.0f / rl;
-        uint16_t *to = (uint16_t *)a.out + token * a.out_stride + (uint64_t)h * D + at;
-        uint32_t w[DT / 2];
-#pragma unroll
-        for (uint32_t d = 0; d < DT; d += 2) w[d / 2] = float_elem<T>(o[d] * inverse) | float_elem<T>(o[d + 1] * inverse) << 16;
-        if constexpr (DT == 8) *reinterpret_cast<u32x4 *>(to) = u32x4{w[0], w[1], w[2], w[3]};
-        else {
-            Words2<8> v;
-            v.w[0] = w[0];
-            v.w[1] = w[1];
-            *reinterpret_cast<Words2<8> *>(to) = v;
-        }
-    };
-
     if constexpr (TOKEN_WAVES == 1) {
+        // register e of a lane: elements (4 g + e) D / 16 .. of row l of each tile
 #pragma unroll
-        for (int i = 0; i < NR; ++i)
+        for (int i = 0; i < NR; ++i) {
+            const uint32_t r = r0 + 16 * i + l;
+            if (r >= rows) continue;
+            const uint64_t token = sq.first + r / a.group, h = head * a.group + r % a.group;
+            if (direct) {
+                const float inverse = sum[i] == 0.0f ? 0.0f : 1.0f / sum[i];
+                uint16_t *const to = (uint16_t *)a.out + token * a.out_stride + h * D + 4 * g * DT;
 #pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) {
-                float o[DT];
+                for (uint32_t e = 0; e < 4; ++e)
 #pragma unroll
-                for (uint32_t d = 0; d < DT; ++d) o[d] = acc[i][d][e];
-                store(r0 + 16 * i + l, e, o, m[i], sum[i][0]);
+                    for (uint32_t d = 0; d < DT; d += 4) {
+                        Words2<8> w;
+                        w.w[0] = float_elem<T>(acc[i][d][e] * inverse) | float_elem<T>(acc[i][d + 1][e] * inverse) << 16;
+                        w.w[1] = float_elem<T>(acc[i][d + 2][e] * inverse) | float_elem<T>(acc[i][d + 3][e] * inverse) << 16;
+                        *reinterpret_cast<Words2<8> *>(to + e * DT + d) = w;
+                    }
+            } else {
+                const uint64_t row = ((uint64_t)split * a.c.tokens + token) * a.heads + h;
+                if (g == 0) a.stat[row] = f32x2{m[i], sum[i]};
+                float *const to = a.part + row * D + 4 * g * DT;
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+#pragma unroll
+                    for (uint32_t d = 0; d < DT; d += 4) *reinterpret_cast<f32x4 *>(to + e * DT + d) = f32x4{acc[i][d][e], acc[i][d + 1][e], acc[i][d + 2][e], acc[i][d + 3][e]};
             }
+        }
     } else {
-        // the wavefronts' parts of the same rows meet in LDS: rows are D + 4 numbers apart
+        // the wavefronts' parts of the same rows meet in LDS, a tile after the other: rows are D + 4 numbers apart
 #pragma unroll
         for (int i = 0; i < NR; ++i)
-            if (g == 0) lds_stat[wave * 16 * NR + 16 * i + l] = f32x2{m[i], sum[i][0]};
+            if (g == 0) lds_stat[wave * 16 * NR + 16 * i + l] = f32x2{m[i], sum[i]};
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
+            if (i) __syncthreads();
             float top = LOWEST;
 #pragma unroll
             for (uint32_t w = 0; w < TOKEN_WAVES; ++w) top = fmaxf(top, lds_stat[w * 16 * NR + 16 * i + l][0]);
             const float factor = __builtin_amdgcn_exp2f(m[i] - top);
-            float *to = lds + (wave * 16 * NR + 16 * i + l) * (D + 4);
+            float *const part = lds + (wave * 16 + l) * (D + 4);
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e)
 #pragma unroll
                 for (uint32_t d = 0; d < DT; d += 4)
-                    *reinterpret_cast<f32x4 *>(to + (4 * g + e) * DT + d) = f32x4{acc[i][d][e] * factor, acc[i][d + 1][e] * factor, acc[i][d + 2][e] * factor, acc[i][d + 3][e] * factor};
-        }
-        __syncthreads();
-        // wavefront w joins register e = w of all
+                    *reinterpret_cast<f32x4 *>(part + (4 * g + e) * DT + d) = f32x4{acc[i][d][e] * factor, acc[i][d + 1][e] * factor, acc[i][d + 2][e] * factor, acc[i][d + 3][e] * factor};
+            __syncthreads();
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            float top = LOWEST, total = 0.0f, o[DT];
+            for (uint32_t x = threadIdx.x; x < 16 * (D / 4); x += 64 * WAVES) {
+                const uint32_t in = x / (D / 4), at = 4 * (x % (D / 4)), r = r0 + 16 * i + in;
+                if (r >= rows) continue;
+                float most = LOWEST, total = 0.0f;
+                f32x4 o = {0, 0, 0, 0};
 #pragma unroll
-            for (uint32_t w = 0; w < TOKEN_WAVES; ++w) top = fmaxf(top, lds_stat[w * 16 * NR + 16 * i + l][0]);
+                for (uint32_t w = 0; w < TOKEN_WAVES; ++w) most = fmaxf(most, lds_stat[w * 16 * NR + 16 * i + in][0]);
 #pragma unroll
-            for (uint32_t w = 0; w < TOKEN_WAVES; ++w) {
-                const f32x2 st = lds_stat[w * 16 * NR + 16 * i + l];
-                total += st[1] * __builtin_amdgcn_exp2f(st[0] - top);
+                for (uint32_t w = 0; w < TOKEN_WAVES; ++w) {
+                    const f32x2 st = lds_stat[w * 16 * NR + 16 * i + in];
+                    total += st[1] * __builtin_amdgcn_exp2f(st[0] - most);
+                    o += *reinterpret_cast<const f32x4 *>(lds + (w * 16 + in) * (D + 4) + at);
+                }
+                const uint64_t token = sq.first + r / a.group, h = head * a.group + r % a.group;
+                if (direct) {
+                    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+                    Words2<8> w;
+                    w.w[0] = float_elem<T>(o[0] * inverse) | float_elem<T>(o[1] * inverse) << 16;
+                    w.w[1] = float_elem<T>(o[2] * inverse) | float_elem<T>(o[3] * inverse) << 16;
+                    *reinterpret_cast<Words2<8> *>((uint16_t *)a.out + token * a.out_stride + h * D + at) = w;
+                } else {
+                    const uint64_t row = ((uint64_t)split * a.c.tokens + token) * a.heads + h;
+                    if (at == 0) a.stat[row] = f32x2{most, total};
+                    *reinterpret_cast<f32x4 *>(a.part + row * D + at) = o;
+                }
             }
-#pragma unroll
-            for (uint32_t d = 0; d < DT; d += 4) {
-                f32x4 v = {0, 0, 0, 0};
-#pragma unroll
-                for (uint32_t w = 0; w < TOKEN_WAVES; ++w) v += *reinterpret_cast<const f32x4 *>(lds + (w * 16 * NR + 16 * i + l) * (D + 4) + (4 * g + wave) * DT + d);
-                o[d] = v[0]; o[d + 1] = v[1]; o[d + 2] = v[2]; o[d + 3] = v[3];
-            }
-            const uint32_t r = r0 + 16 * i + l;
-            store(r, wave, o, top, total);
         }
     }
 }
 
-// The splits' parts of a row, joined: a wavefront per row.
-template <int T, int D> __global__ void __launch_bounds__(256) attention_join_kernel(const AttentionArgs a, uint32_t block_rows, uint32_t least)
+// The parts of a row, joined, where there are several: a wavefront per row, AT_ONCE parts on their way at once.
+template <int T, int D, uint32_t AT_ONCE> __global__ void __launch_bounds__(256) attention_join_kernel(const AttentionArgs a, uint32_t block_rows)
 {
+    constexpr uint32_t PER = D / 64;
     const uint32_t lane = threadIdx.x & 63u;
     const uint32_t r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);              // row: token, then head
     const Sequence sq = sequence_of(a.c, blockIdx.y);
     const uint32_t n = sq.n < a.max_tokens ? sq.n : a.max_tokens, i = r / a.heads, h = r % a.heads;
     if (i >= n) return;
     const uint32_t in_head = i * a.group + h % a.group;
-    const Range range = granules_of(a, sq, in_head / block_rows * block_rows, block_rows, least);
-    const uint32_t parts = (range.count + range.chunk - 1) / range.chunk;          // at most 64
+    const uint32_t parts = granules_of(a, sq, in_head / block_rows * block_rows, block_rows).parts;    // at most 64
+    if (parts == 1) return;
     const uint64_t row = (uint64_t)(sq.first + i) * a.heads + h, apart = (uint64_t)a.c.tokens * a.heads;
+    const float *const from = a.part + row * D + lane * PER;
     f32x2 st = {LOWEST, 0.0f};
     if (lane < parts) st = a.stat[lane * apart + row];
-    float top = st[0];
+    float o[PER] = {}, top = LOWEST, factor = 0.0f;
+    for (uint32_t z0 = 0; z0 < parts; z0 += AT_ONCE) {
+        float x[AT_ONCE][PER];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    const float factor = __builtin_amdgcn_exp2f(st[0] - top);
+        for (uint32_t z = 0; z < AT_ONCE; ++z) {
+            const float *const p = from + (z0 + z < parts ? z0 + z : z0) * apart * D;
+#pragma unroll
+            for (uint32_t d = 0; d < PER; ++d) x[z][d] = p[d];
+        }
+        if (z0 == 0) {
+            top = st[0];
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+            factor = __builtin_amdgcn_exp2f(st[0] - top);
+        }
+#pragma unroll
+        for (uint32_t z = 0; z < AT_ONCE; ++z) {
+            if (z0 + z >= parts) break;
+            const float f = __shfl(factor, (int)(z0 + z));
+#pragma unroll
+            for (uint32_t d = 0; d < PER; ++d) o[d] += f * x[z][d];
+        }
+    }
     float total = st[1] * factor;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
-    float o[D / 64] = {};
-    for (uint32_t z = 0; z < parts; ++z) {
-        const float f = __shfl(factor, (int)z);
-        const float *from = a.part + (z * apart + row) * D + lane * (D / 64);
-#pragma unroll
-        for (int d = 0; d < D / 64; ++d) o[d] += f * from[d];
-    }
     const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
-    uint16_t *to = (uint16_t *)a.out + (uint64_t)(sq.first + i) * a.out_stride + (uint64_t)h * D + lane * (D / 64);
+    uint16_t *to = (uint16_t *)a.out + (uint64_t)(sq.first + i) * a.out_stride + (uint64_t)h * D + lane * PER;
     if constexpr (D == 128) *reinterpret_cast<uint32_t *>(to) = float_elem<T>(o[0] * inverse) | float_elem<T>(o[1] * inverse) << 16;
     else *to = (uint16_t)float_elem<T>(o[0] * inverse);
 }
 
-// ---- which shape, and how many splits ------------------------------------------------------
-struct Plan { uint32_t nr, row_waves, block_rows, blocks, splits, least; };
+// ---- which shape, and how many parts ---------------------------------------------------------
+struct Plan { uint32_t nr, row_waves, waves, block_rows, blocks, splits, chunk; };
 
 static Plan plan_of(const mmaemu_attention_fp4_args &a)
 {
     const uint32_t rows = a.max_tokens * (a.heads / a.kv_heads);
     Plan p;
-    p.nr = rows <= 16 ? 1 : rows <= 64 ? 2 : 4;
     p.row_waves = rows <= 64 ? 1 : 4;
+    p.nr = rows <= 64 ? (rows + 15) / 16 : 3;
     p.block_rows = 16 * p.nr * p.row_waves;
     p.blocks = (rows + p.block_rows - 1) / p.block_rows;
-    p.least = 2 * (4 / p.row_waves);
     const uint64_t groups = (uint64_t)p.blocks * a.kv_heads * a.sequences;
+    p.waves = p.row_waves == 1 && groups <= 32 ? 8 : 4;
     const uint64_t seen = a.window && (uint64_t)a.window + a.max_tokens < a.max_length ? (uint64_t)a.window + a.max_tokens : a.max_length;
-    const uint64_t most = (seen + 31) / 32 / p.least;
-    uint64_t splits = groups ? 1024 / groups : 1;
-    if (splits > most) splits = most;
+    const uint64_t granules = (seen + 31) / 32, least = p.row_waves == 1 ? 4 * p.waves : 32;
+    const uint64_t target = p.waves == 8 ? 256 : 1024;
+    uint64_t splits = groups ? target / groups : 1;
+    if (splits > granules / least) splits = granules / least;
     p.splits = splits < 1 ? 1 : splits > 64 ? 64 : (uint32_t)splits;
+    p.chunk = (uint32_t)((granules + p.splits - 1) / p.splits);
+    if (p.chunk < 1) p.chunk = 1;
     return p;
 }
 
@@ -461,13 +523,26 @@ uint64_t attention_fp4_workspace(const mmaemu_attention_fp4_args &a)
 template <int T, int D> static mmaemu_status launch_typed(const AttentionArgs &p, const Plan &plan, hipStream_t s)
 {
     const dim3 grid(plan.blocks * p.c.kv_heads, plan.splits, p.c.sequences);
-    if (plan.row_waves == 4) hipLaunchKernelGGL((attention_kernel<T, D, 4, 4>), grid, dim3(256), 0, s, p);
-    else if (plan.nr == 2) hipLaunchKernelGGL((attention_kernel<T, D, 2, 1>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((attention_kernel<T, D, 1, 1>), grid, dim3(256), 0, s, p);
+#define MMAEMU_ATTENTION(NR, ROW_WAVES, WAVES) hipLaunchKernelGGL((attention_kernel<T, D, NR, ROW_WAVES, WAVES>), grid, dim3(64 * WAVES), 0, s, p)
+#define MMAEMU_ATTENTION_TOKENS(NR)                          \
+    do {                                                     \
+        if (plan.waves == 8) MMAEMU_ATTENTION(NR, 1, 8);     \
+        else MMAEMU_ATTENTION(NR, 1, 4);                     \
+    } while (0)
+    if (plan.row_waves == 4) MMAEMU_ATTENTION(3, 4, 4);
+    else if (plan.nr == 1) MMAEMU_ATTENTION_TOKENS(1);
+    else if (plan.nr == 2) MMAEMU_ATTENTION_TOKENS(2);
+    else if (plan.nr == 3) MMAEMU_ATTENTION_TOKENS(3);
+    else MMAEMU_ATTENTION_TOKENS(4);
+#undef MMAEMU_ATTENTION_TOKENS
+#undef MMAEMU_ATTENTION
     MMAEMU_HIP(hipGetLastError());
     if (plan.splits > 1) {
         const uint64_t rows = (uint64_t)p.max_tokens * p.heads;
-        hipLaunchKernelGGL((attention_join_kernel<T, D>), dim3((uint32_t)((rows + 3) / 4), p.c.sequences), dim3(256), 0, s, p, plan.block_rows, plan.least);
+        const dim3 join((uint32_t)((rows + 3) / 4), p.c.sequences);
+        if (plan.splits <= 4) hipLaunchKernelGGL((attention_join_kernel<T, D, 4>), join, dim3(256), 0, s, p, plan.block_rows);
+        else if (plan.splits <= 16) hipLaunchKernelGGL((attention_join_kernel<T, D, 16>), join, dim3(256), 0, s, p, plan.block_rows);
+        else hipLaunchKernelGGL((attention_join_kernel<T, D, 32>), join, dim3(256), 0, s, p, plan.block_rows);
         MMAEMU_HIP(hipGetLastError());
     }
     return MMAEMU_OK;
@@ -476,8 +551,8 @@ template <int T, int D> static mmaemu_status launch_typed(const AttentionArgs &p
 mmaemu_status launch_attention_fp4(const mmaemu_attention_fp4_args &a, const CacheArgs &c, hipStream_t s)
 {
     const Plan plan = plan_of(a);
-    AttentionArgs p = {c, a.q, a.out, (float *)a.workspace, nullptr, a.q_stride, a.out_stride, a.heads, a.heads / a.kv_heads, a.max_tokens, a.window, plan.splits,
-                       plan.blocks, (float)(a.scale * 1.4426950408889634)};
+    AttentionArgs p = {c, a.q, a.out, (float *)a.workspace, nullptr, a.q_stride, a.out_stride, a.heads, a.heads / a.kv_heads, a.max_tokens, a.window, plan.blocks,
+                       plan.splits, plan.chunk, (float)(a.scale * 1.4426950408889634)};
     p.stat = (f32x2 *)(p.part + (uint64_t)plan.splits * a.tokens * a.heads * a.dim);
     if (a.type == MMAEMU_BF16) return a.dim == 128 ? launch_typed<MMAEMU_BF16, 128>(p, plan, s) : launch_typed<MMAEMU_BF16, 64>(p, plan, s);
     return a.dim == 128 ? launch_typed<MMAEMU_FP16, 128>(p, plan, s) : launch_typed<MMAEMU_FP16, 64>(p, plan, s);

@@ -53,8 +53,9 @@ def attention_oracle(seqs, q, heads, scale, window=0, max_tokens=None):
     """q: values [tokens][heads][dim].  (outputs, absolute error allowed before the output's own rounding, rows that belong to a sequence).
 
     The kernel's sums: a score is a sum of dim products in binary32 (each step off by at most 2^-23 of the sum of magnitudes), times the
-    scale in units of log2, minus the maximum, plus a shift of ten (steps of 2^-24 of numbers up to their magnitude + 10), its exponential within
-    2^-22; the weight is rounded to FP16 (2^-11; 2^-25 of 2^10 absolute for the smallest); sums over tokens in binary32."""
+    scale in units of log2, minus the maximum, plus a shift of at most ten (steps of 2^-24 of numbers up to their magnitude + 10), its exponential within
+    2^-22; the weight, held times 2^4 or more of the largest, is rounded to FP16: 2^-11 relative, and below its normal numbers half a step of 2^-24, which is 2^-29 of the
+    largest weight and so of their sum; sums over tokens in binary32."""
     d = seqs.dim
     want, room = np.zeros((seqs.tokens, heads, d)), np.zeros((seqs.tokens, heads, d))
     mine = np.zeros(seqs.tokens, dtype=bool)
@@ -69,7 +70,7 @@ def attention_oracle(seqs, q, heads, scale, window=0, max_tokens=None):
         score = (d * 2.0 ** -23 * most + 2.0 ** -23 * (2 * top + 10)) * log2e * 2           # of a score and of the row's maximum, in log2
         weight = np.expm1(score * np.log(2)) + 2.0 ** -22
         want[at] = o
-        room[at] = spread * (2.0 ** -11 + 2 * weight[..., None] + (count[:, None, None] + 64) * 2.0 ** -23) + count[:, None, None] * 2.0 ** -34 * (np.nanmax(np.abs(v), initial=0.0))
+        room[at] = spread * (2.0 ** -11 + 2 * weight[..., None] + (count[:, None, None] + 64) * 2.0 ** -23) + count[:, None, None] * 2.0 ** -29 * (np.nanmax(np.abs(v), initial=0.0))
     return want, room, mine
 
 

@@ -5,48 +5,9 @@
 //   s = scale log2(e) q.k;  m' = max(m, max s);  p = 2^(s - m');  l = l 2^(m - m') + sum p;  O = O 2^(m - m') + p V;  out = O / l
 // Both products are 16 x 16 x 32 instructions on operands that lie in the cache as the lanes take them (cache_fp4.hpp), brought to 16 bits, which is
 // exact: K to the queries' type, V to FP16.  The scores' registers are the second product's operand as they are, rounded to FP16.
-#include "cache_fp4.hpp"
-#include "fp4_operands.hpp"
+#include "attention_fp4.hpp"
 
 namespace mmaemu {
-
-struct AttentionArgs {
-    CacheArgs c;
-    const void *q;
-    void *out;
-    float *part;                                   // [split][token][head][D], unnormalised, and behind them
-    f32x2 *stat;                                   // [split][token][head] (m, l)
-    uint64_t q_stride, out_stride;
-    uint32_t heads, group, max_tokens, window, blocks;                 // blocks: of rows, of a sequence's KV head
-    uint32_t splits, chunk;                        // most workgroups that share a row's granules, and how many granules make one more worth it
-    float c2;                                      // scale log2(e)
-};
-
-constexpr float LOWEST = -3.0e38f;                 // a maximum over nothing
-// Weights are held times 2^SHIFT, relative to a maximum that moves where those of a granule come to LIMIT together: it may lie 2^11 below.  Weights down to 2^-18
-// of the largest keep FP16's eleven bits, and smaller ones are off by 2^-29 of it at most.
-constexpr float SHIFT = 4.0f, LIMIT = 32768.0f;
-
-// The granules that the rows r0 .. of a block see, and the parts that workgroups take of them, `chunk` each.
-struct Range { uint32_t first, count, parts, chunk; };
-__device__ __forceinline__ Range granules_of(const AttentionArgs &a, const Sequence &sq, uint32_t r0, uint32_t rows)
-{
-    const uint32_t all = (sq.n < a.max_tokens ? sq.n : a.max_tokens) * a.group;
-    const uint32_t last = (r0 + rows < all ? r0 + rows : all) - 1;
-    const int32_t p0 = sq.start + (int32_t)(r0 / a.group), end = sq.start + (int32_t)(last / a.group) + 1;
-    const int32_t begin = a.window && (uint32_t)(p0 < 0 ? 0 : p0) >= a.window ? p0 + 1 - (int32_t)a.window : 0;
-    Range g;
-    g.first = (uint32_t)begin / 32u;
-    g.count = end > begin ? ((uint32_t)end + 31u) / 32u - g.first : 0u;
-    g.parts = 1;
-    g.chunk = g.count;
-    if (a.splits > 1) {
-        g.parts = (g.count + a.chunk - 1) / a.chunk;
-        g.parts = g.parts < 1 ? 1u : g.parts > a.splits ? a.splits : g.parts;
-        g.chunk = (g.count + g.parts - 1) / g.parts;
-    }
-    return g;
-}
 
 __device__ __forceinline__ float other_rows_max(float x)               // over lanes l, l + 16, l + 32, l + 48
 {
@@ -88,70 +49,15 @@ template <int D> __device__ __forceinline__ void load_values(Values<D> &x, const
     x.scales[1] = w.w[1];
 }
 
-// The conversions read the exponent field of their scale alone (all 256 fields with other bits around them: no difference), so a code needs no more than
-// to be shifted there.
-template <int BYTE> __device__ __forceinline__ float scale_of(uint32_t codes)
-{
-    return __uint_as_float(BYTE == 0 ? codes << 23 : BYTE == 1 ? codes << 15 : BYTE == 2 ? codes << 7 : codes >> 1);
-}
-__device__ __forceinline__ Frag16 keys_bf16(uint32_t codes, float s)
-{
-    Frag16 f;
-    f.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0));
-    f.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1));
-    f.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2));
-    f.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3));
-    return f;
-}
-__device__ __forceinline__ Frag16 keys_fp16(uint32_t codes, float s)
-{
-    Frag16 f;
-    f.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 0));
-    f.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 1));
-    f.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 2));
-    f.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 3));
-    return f;
-}
 // the 16-bit K operand of half A, elements 8 j .. 8 j + 7 of the lane's D / 4
 template <int T, int D, int A> __device__ __forceinline__ Frag16 k_operand(const Keys<D> &x, int j)
 {
     const uint32_t word = D == 128 ? x.k[D == 128 ? A : 0][j] : x.k[0][2 * A + j];
     return T == MMAEMU_BF16 ? keys_bf16(word, scale_of<A>(x.scales)) : keys_fp16(word, scale_of<A>(x.scales));
 }
-// two elements of tokens 4 H .. 4 H + 3, a byte each, under those tokens' scales
-template <int H> __device__ __forceinline__ void four_values(uint32_t word, const uint32_t (&scales)[2], f16x2 (&y)[8])
-{
-    y[4 * H] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_of<0>(scales[H]), 0);
-    y[4 * H + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_of<1>(scales[H]), 1);
-    y[4 * H + 2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_of<2>(scales[H]), 2);
-    y[4 * H + 3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_of<3>(scales[H]), 3);
-}
-
-// codes of bytes 0xFF in a word, as 0x80 in their bytes (exact: the lowest byte that is one is found, and those above it)
-__device__ __forceinline__ uint32_t any_nan_code(uint32_t w) { return (~w - 0x01010101u) & w & 0x80808080u; }
-
-// The pages of a wavefront's granules: granules `at`, `at` + step, ... of the sequence, 64 entries of the table at a time, one a lane.
-template <int D> struct Walk {
-    const uint8_t *base;                           // of the head in page 0
-    const int32_t *row;
-    uint64_t page_bytes;
-    uint32_t pages, page_granules, at, step, lane;
-    int32_t entry;
-    __device__ __forceinline__ Walk(const CacheArgs &c, uint32_t sequence, uint32_t head, uint32_t first, uint32_t step_, uint32_t lane_)
-        : base(c.cache + (uint64_t)head * c.page_granules * (34 * D)), row(c.table + sequence * c.table_stride), page_bytes((uint64_t)c.kv_heads * c.page_granules * (34 * D)),
-          pages(c.pages), page_granules(c.page_granules), at(first), step(step_), lane(lane_), entry(-1) {}
-    // the entries for the next 64 of the `left` granules still to come
-    __device__ __forceinline__ void refill(uint32_t n, uint32_t left) { entry = lane < left ? row[(at + (n + lane) * step) / page_granules] : -1; }
-    // granule n of the walk; NULL where its page is none
-    __device__ __forceinline__ const uint8_t *granule(uint32_t n) const
-    {
-        const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(entry, (int)(n & 63u)), g = (at + n * step) % page_granules;
-        return page < pages ? base + page * page_bytes + g * (34 * D) : nullptr;
-    }
-};
 
 // Rows of NR x 16 x ROW_WAVES, tokens split over the other wavefronts.  Where the tiles of rows are many, the queries wait in LDS.
-template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __launch_bounds__(64 * WAVES, NR == 1 ? 4 : D == 64 ? (NR == 2 ? 4 : NR == 3 ? 3 : 2) : 2) attention_kernel(const AttentionArgs a)
+template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __launch_bounds__(64 * WAVES, NR == 1 || (NR == 2 && D == 64) ? 4 : NR == 2 || D == 64 ? 3 : 2) attention_kernel(const AttentionArgs a)
 {
     constexpr uint32_t TOKEN_WAVES = WAVES / ROW_WAVES, J = D / 32, DT = D / 16;
     constexpr uint32_t ROWS = 16 * NR * ROW_WAVES;
@@ -492,20 +398,39 @@ template <int T, int D, uint32_t AT_ONCE> __global__ void __launch_bounds__(256)
 // ---- which shape, and how many parts ---------------------------------------------------------
 struct Plan { uint32_t nr, row_waves, waves, block_rows, blocks, splits, chunk; };
 
+// Up to 64 rows of a KV head (a token's, a few drafts'): one workgroup has them all, its wavefronts share the tokens.  Eight wavefronts where workgroups are few (one
+// sequence, 513 tokens: 6.5 us, 7.5 with four; 131072 tokens: 31 and 33), four else (24 sequences of 35 rows: 21 and 23).  Parts: as many as fill the chip once (eight wavefronts)
+// or four times, none below four granules a wavefront: 64 sequences of up to 16384 tokens 173 us in one part, 147 in two, 152 in eight; one of 131072 47 us in 16 parts, 31 in 32.
+//
+// More rows: four wavefronts of `nr` tiles each.  The more tiles, the fewer conversions a row costs, but the fewer workgroups there are: the choice goes by the granules that all
+// workgroups of three tiles would see, us with one, two and three tiles: 1500 tokens x 32 heads (6000 granules) 43, 50 and 58; 3000 (24000) 115, 109 and 112; 500 over 8000
+// (21000) 122, 104 and 117; 8192 (176000) 585 with two, 543 with three.  Parts where a row sees much more than comes with the call, or the blocks' order, longest first, would not even
+// them out: so that few blocks fill the chip once (100 tokens over 8000: 180 us in one part, 44 in eight; 500: 222 and 104 in four), and many are cut
+// small enough, but not below 24 granules (six sequences of up to 1030 over 6007: 410 us in one part, 378 in three; four of up to 500 over 2500: 93 in two, 111 in six).  A prompt by itself takes 543 us in one part and 646 in two.
 static Plan plan_of(const mmaemu_attention_fp4_args &a)
 {
-    const uint32_t rows = a.max_tokens * (a.heads / a.kv_heads);
-    Plan p;
-    p.row_waves = rows <= 64 ? 1 : 4;
-    p.nr = rows <= 64 ? (rows + 15) / 16 : 3;
-    p.block_rows = 16 * p.nr * p.row_waves;
-    p.blocks = (rows + p.block_rows - 1) / p.block_rows;
-    const uint64_t groups = (uint64_t)p.blocks * a.kv_heads * a.sequences;
-    p.waves = p.row_waves == 1 && groups <= 32 ? 8 : 4;
+    const uint32_t group = a.heads / a.kv_heads, rows = a.max_tokens * group;
     const uint64_t seen = a.window && (uint64_t)a.window + a.max_tokens < a.max_length ? (uint64_t)a.window + a.max_tokens : a.max_length;
-    const uint64_t granules = (seen + 31) / 32, least = p.row_waves == 1 ? 4 * p.waves : 32;
-    const uint64_t target = p.waves == 8 ? 256 : 1024;
-    uint64_t splits = groups ? target / groups : 1;
+    const uint64_t granules = (seen + 31) / 32, heads = (uint64_t)a.kv_heads * a.sequences;
+    Plan p;
+    uint64_t splits, least;
+    if (rows <= 64) {
+        p.row_waves = 1;
+        p.nr = (rows + 15) / 16;
+        p.blocks = 1;
+        p.waves = heads <= 32 ? 8 : 4;
+        splits = heads ? (p.waves == 8 ? 256 : 1024) / heads : 1;
+        least = 4 * p.waves;
+    } else {
+        p.row_waves = p.waves = 4;
+        const uint64_t triples = heads * ((rows + 191) / 192), all = triples * (seen >= 2ull * a.max_tokens ? granules : (granules + 1) / 2);
+        p.nr = all <= 20000 ? 1 : all <= 40000 ? 2 : 3;
+        p.blocks = (rows + 64 * p.nr - 1) / (64 * p.nr);
+        const uint64_t groups = heads * p.blocks;
+        splits = seen < 2ull * a.max_tokens || !groups ? 1 : groups <= 256 ? 512 / groups : (2600 + groups - 1) / groups;
+        least = groups <= 256 ? 4 : 24;
+    }
+    p.block_rows = 16 * p.nr * p.row_waves;
     if (splits > granules / least) splits = granules / least;
     p.splits = splits < 1 ? 1 : splits > 64 ? 64 : (uint32_t)splits;
     p.chunk = (uint32_t)((granules + p.splits - 1) / p.splits);
@@ -529,8 +454,11 @@ template <int T, int D> static mmaemu_status launch_typed(const AttentionArgs &p
         if (plan.waves == 8) MMAEMU_ATTENTION(NR, 1, 8);     \
         else MMAEMU_ATTENTION(NR, 1, 4);                     \
     } while (0)
-    if (plan.row_waves == 4) MMAEMU_ATTENTION(3, 4, 4);
-    else if (plan.nr == 1) MMAEMU_ATTENTION_TOKENS(1);
+    if (plan.row_waves == 4) {
+        if (plan.nr == 1) MMAEMU_ATTENTION(1, 4, 4);
+        else if (plan.nr == 2) MMAEMU_ATTENTION(2, 4, 4);
+        else MMAEMU_ATTENTION(3, 4, 4);
+    } else if (plan.nr == 1) MMAEMU_ATTENTION_TOKENS(1);
     else if (plan.nr == 2) MMAEMU_ATTENTION_TOKENS(2);
     else if (plan.nr == 3) MMAEMU_ATTENTION_TOKENS(3);
     else MMAEMU_ATTENTION_TOKENS(4);

@@ -21,8 +21,8 @@ struct AppendArgs {
     const float *rotation;
     void *q_out, *k_values, *v_values;
     uint64_t q_stride, k_stride, v_stride, q_out_stride;
-    uint32_t heads, kv_read, vectors;              // vectors: heads of q, k and v of a token
-    uint32_t units, per;                           // wavefronts that share a token or group, and the vectors (one after another) of each
+    uint32_t heads, kv_read, per;                  // per: heads that a wavefront takes one after another
+    uint32_t units, q_units, kv_units;             // wavefronts that share a token or group of tokens, for queries, and for keys or values
     uint32_t max_tokens, rotary, pairs, fit, rotation_rows;
     double eps;
 };
@@ -95,22 +95,17 @@ template <int T, int TW, int D, bool HEADS> __global__ void __launch_bounds__(25
     const uint32_t wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = wave % a.units, nth = wave / a.units;
     const Sequence sq = sequence_of(a.c, blockIdx.y);
     const uint32_t n = sq.n < a.max_tokens ? sq.n : a.max_tokens;
-    // the lane's token, and the wavefront's vectors: heads of q, then k, then v (HEADS: GROUPS of them at once, each kind by itself)
+    // the lane's token
     int32_t first = 0;
-    uint32_t begin, end;
     bool here;
     int32_t i;
     if (HEADS) {
         i = (int32_t)nth;
         here = nth < n;
-        begin = share;
-        end = share + 1;
     } else {
         first = ((sq.start >= 0 ? sq.start : sq.start - (int32_t)(GROUPS - 1)) / (int32_t)GROUPS + (int32_t)nth) * (int32_t)GROUPS;
         i = first + (int32_t)tt - sq.start;
         here = i >= 0 && (uint32_t)i < n;
-        begin = share * a.per;
-        end = begin + a.per < a.vectors ? begin + a.per : a.vectors;
     }
     if (!__any(here)) return;
     const int32_t position = sq.start + i;
@@ -131,11 +126,11 @@ template <int T, int TW, int D, bool HEADS> __global__ void __launch_bounds__(25
     const float *angles = nullptr;
     if (turns && held) angles = a.rotation + (uint64_t)(uint32_t)position * a.rotary + (a.pairs ? 4 * v : 8 * (upper ? other : v));
 
-    // the wavefront's heads of one kind: vectors x0 .. x1 - 1 of that kind (HEADS: of GROUPS heads)
-    const auto heads_of_kind = [&](auto which, uint32_t x0, uint32_t x1) __attribute__((always_inline)) {
+    // `per` heads of one kind, one after another (HEADS: GROUPS heads at once)
+    const auto heads_of_kind = [&](auto which, uint32_t nth_share) __attribute__((always_inline)) {
         constexpr int kind = decltype(which)::value;
-        if (x0 >= x1) return;
         const uint32_t count = kind == KIND_Q ? a.heads : a.kv_read;
+        const uint32_t x0 = HEADS ? nth_share : nth_share * a.per, x1 = HEADS ? x0 + 1 : x0 + a.per < count ? x0 + a.per : count;
         const void *const from = kind == KIND_Q ? a.q : kind == KIND_K ? a.k : a.v;
         const uint64_t in = row * (kind == KIND_Q ? a.q_stride : kind == KIND_K ? a.k_stride : a.v_stride) + 8 * v;
         const auto head_of = [&](uint32_t x) { return HEADS ? x * GROUPS + tt : x; };
@@ -256,31 +251,25 @@ template <int T, int TW, int D, bool HEADS> __global__ void __launch_bounds__(25
         }
     };
 
-    // vectors of a token: heads of q, then of k, then of v
-    const uint32_t q_units = HEADS ? (a.heads + GROUPS - 1) / GROUPS : a.heads, k_units = HEADS ? (a.kv_read + GROUPS - 1) / GROUPS : a.kv_read;
-    const auto part = [&](auto which, uint32_t first_unit, uint32_t units) __attribute__((always_inline)) {
-        const uint32_t x0 = begin > first_unit ? begin - first_unit : 0u, x1 = end > first_unit ? end - first_unit : 0u;
-        heads_of_kind(which, x0, x1 < units ? x1 : units);
-    };
-    part(std::integral_constant<int, KIND_Q>(), 0, q_units);
-    part(std::integral_constant<int, KIND_K>(), q_units, k_units);
-    part(std::integral_constant<int, KIND_V>(), q_units + k_units, k_units);
+    // the wavefront's share of a token: some heads of q, of k or of v
+    if (share < a.q_units) heads_of_kind(std::integral_constant<int, KIND_Q>(), share);
+    else if (share < a.q_units + a.kv_units) heads_of_kind(std::integral_constant<int, KIND_K>(), share - a.q_units);
+    else heads_of_kind(std::integral_constant<int, KIND_V>(), share - a.q_units - a.kv_units);
 }
 
 mmaemu_status launch_cache_append(const mmaemu_cache_append_fp4_args &a, const CacheArgs &c, hipStream_t s)
 {
-    const uint32_t kv_read = a.k ? c.kv_heads : 0, vectors = a.heads + 2 * kv_read, groups = a.dim == 128 ? 4 : 8;
+    const uint32_t kv_read = a.k ? c.kv_heads : 0, groups = a.dim == 128 ? 4 : 8;
     const bool by_heads = a.max_tokens <= 2, wide = a.weight_type == MMAEMU_FP32;
     // groups of positions that max_tokens consecutive ones may touch
     const uint32_t parts = by_heads ? a.max_tokens : (a.max_tokens + groups - 2) / groups + 1;
-    uint32_t per = 1, units = (a.heads + groups - 1) / groups + 2 * ((kv_read + groups - 1) / groups);
-    if (!by_heads) {
-        const uint64_t all = (uint64_t)parts * vectors * a.sequences;
-        per = all >= 65536 ? 6 : all >= 32768 ? 3 : 1;
-        units = (vectors + per - 1) / per;
-    }
+    // Heads of a wavefront, us (8192 tokens of 32 + 2 x 8 heads of 128; five chunks of up to 1499 tokens, 12 + 2 x 4 of 64): one 11.6 for the latter, two 66 and 10.5,
+    // four 55 and 11.5, eight 52 and 13, twelve 53 and 12.6
+    const uint64_t all = (uint64_t)parts * (a.heads + 2 * kv_read) * a.sequences;
+    const uint32_t per = by_heads ? 1 : all >= 65536 ? 8 : all >= 8192 ? 2 : 1, at_once = by_heads ? groups : per;
+    const uint32_t q_units = (a.heads + at_once - 1) / at_once, kv_units = (kv_read + at_once - 1) / at_once, units = q_units + 2 * kv_units;
     const AppendArgs p = {c, a.q, a.k, a.v, a.q_weight, a.k_weight, a.rotation, a.q_out, a.k_values, a.v_values, a.q_stride, a.k_stride, a.v_stride, a.q_out_stride,
-                          a.heads, kv_read, vectors, units, per, a.max_tokens, a.rotary_dim, a.rotation_style == MMAEMU_ROTATE_PAIRS,
+                          a.heads, kv_read, per, units, q_units, kv_units, a.max_tokens, a.rotary_dim, a.rotation_style == MMAEMU_ROTATE_PAIRS,
                           a.scale_rule == MMAEMU_SCALE_RULE_FIT, (uint32_t)(a.rotation_rows < 0x7FFFFFFF ? a.rotation_rows : 0x7FFFFFFF), a.eps};
     const dim3 grid((parts * units + 3) / 4, a.sequences);
 #define MMAEMU_APPEND(T, TW, D)                                                                                       \

@@ -686,13 +686,15 @@ mmaemu_status mmaemu_cache_append_fp4(const mmaemu_cache_append_fp4_args *args);
  *   out[r][h] = sum over t of p_t v_t,  p = softmax over t of scale * (q[r][h] . k_t),  k and v of head h / (heads / kv_heads),
  * over the tokens t <= position of row r, and > position - window where window is not 0.  A row that sees no token gives zeros.  Tokens that a row does not
  * see have no part in it, whatever they hold.
- * Scores, maxima and sums are binary32; the weights p, relative to a maximum, are rounded to FP16 (nearest even) for the second product.
+ * Scores, maxima and sums are binary32; the weights p, relative to a maximum that may lie 2^11 below the largest, are rounded to FP16 (nearest even) for the
+ * second product: those below 2^-18 of the row's largest are off by up to 2^-29 of it.  A score that leaves binary32 is an infinity: tokens of minus infinity
+ * weigh nothing, a row with one of plus infinity is NaN.
  * max_length: the host's bound for lengths; it decides, with the other sizes, over how many workgroups a row's tokens are split, and nothing
  * else (longer sequences are computed all the same).  workspace: device memory of mmaemu_attention_fp4_workspace bytes, 16-byte aligned, for one call at a
  * time: calls that share it have to follow one another, those in graphs too.  NULL where that is 0.  One launch, or two where rows are split.  Results do
  * not depend on anything but the call's arguments and data.  out may be q where strides are equal; no other arrays may overlap.  Forward only.
- * Errors: as above; SHAPE (heads no multiple of kv_heads, max_tokens * heads / kv_heads above 2^24), INVALID_ARG (scale not positive and finite, workspace missing,
- *         misaligned or too small).
+ * Errors: as above; SHAPE (heads 0 or no multiple of kv_heads, max_tokens * heads / kv_heads above 2^24, max_tokens * heads above 2^28), INVALID_ARG (scale outside
+ *         1e-30 .. 1e30, workspace missing, misaligned or too small, out = q under another stride).
  */
 typedef struct {
     uint32_t struct_size, type, dim, heads, kv_heads, page_tokens, sequences, max_tokens, max_length, window;

@@ -121,6 +121,7 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
     // The next granule's keys are read once this one's are used, its values once this one's are: they are on their way during the other's products.
     // (Where a page is none, and past the end, the first granule of the memory is read: a load that always happens costs no branch.)
     bool there = false;
+    float c2 = a.c2;                               // NaN once a maximum has come to FAR: all granules' weights are then made again
     const uint8_t *at = walk.base;
     const auto advance = [&](uint32_t n) MMAEMU_INLINE {
         if ((n & 63u) == 0 && n && n < mine) walk.refill(n, mine - n);
@@ -195,8 +196,8 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
                 const float off = SHIFT - m[i];
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    const f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4], a.c2, off)),
-                                     __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4 + 1], a.c2, off))};
+                    const f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4], c2, off)),
+                                     __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4 + 1], c2, off))};
                     p[i].w[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
                 }
                 total[i] = mfma_fp16(ones, p[i], f32x4{0, 0, 0, 0});
@@ -208,6 +209,7 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
                 over = over || !(add[i] < LIMIT);
             }
             if (moved || !__any(over)) break;
+            bool far = false;
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
                 if (!__any(!(add[i] < LIMIT))) continue;
@@ -219,7 +221,23 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
                 sum[i] *= factor;
 #pragma unroll
                 for (uint32_t d = 0; d < DT; ++d) acc[i][d] *= factor;
+                far = far || (fabsf(top) >= FAR && top != LOWEST);
             }
+            if (__any(far)) c2 = __builtin_nanf("");
+            if (c2 == a.c2) continue;
+            // each score rounded as its maximum was
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+#pragma clang fp contract(off)
+                    const float x0 = sc[i][e / 4][e % 4] * a.c2, x1 = sc[i][e / 4][e % 4 + 1] * a.c2;
+                    const f32x2 y = {__builtin_amdgcn_exp2f(x0 - m[i] + SHIFT), __builtin_amdgcn_exp2f(x1 - m[i] + SHIFT)};
+                    p[i].w[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
+                }
+                add[i] = mfma_fp16(ones, p[i], f32x4{0, 0, 0, 0})[0];
+            }
+            break;
         }
 #pragma unroll
         for (int i = 0; i < NR; ++i) sum[i] += add[i];

@@ -251,6 +251,25 @@ def test_attention_over_long_caches(d, fresh, length, window):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("empty", [290, 650])
+@pytest.mark.parametrize("window", [0, 40, 1300])
+def test_attention_of_chunks_among_many_sequences(d, empty, window):
+    """Chunks over long caches in a batch whose other sequences bring nothing: wavefronts of two and three tiles of rows, in one part and in two."""
+    def alter(s, k, v):
+        if s == 1:
+            v[3, 0], k[9, 1, 3], v[-1, 1, :32] = np.nan, np.nan, np.inf
+    fresh, lengths = [48, 45, 17, 1, 48] + [0] * empty, [1536, 800, 1500, 900, 1530] + [0] * empty
+    seqs = Sequences(empty, fresh, lengths, d, 2, 64).fill(alter)
+    seqs.table[4, 1] = -1
+    shape = seqs.shape(8)
+    # (two parts; the plan counts a window's tokens where they are fewer)
+    size = mm.attention_fp4_workspace(mm.BF16, max_length=1536, window=window, **shape)
+    assert size == (2 * seqs.tokens * 8 * (d + 2) * 4 if window == 0 else 0)
+    run_attention(seqs, 8, mm.BF16, window=window, pad=8)
+    run_attention(seqs, 8, mm.FP16, window=window, in_place=True, max_length=100000)
+
+
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("fresh", [1, 6, 50])
 def test_attention_does_not_see_what_is_not_there(d, fresh):
     """Keys and values that are NaN: outputs are NaN where a row sees them (values: in their block alone), and nowhere else."""
@@ -295,6 +314,47 @@ def test_attention_of_extreme_queries(d):
     q[7, :, 0] = np.inf
     got = run_attention(seqs, 4, mm.FP16, bs.bits_of(np.where(np.isinf(q), np.nan, q), mm.FP16))
     assert got is not None
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("fresh,length", [(1, 1), (1, 2100), (5, 70), (70, 70), (70, 2200)])
+@pytest.mark.parametrize("magnitude", [2.0 ** 12, 2.0 ** 22, 2.0 ** 24, 2.0 ** 31, 2.0 ** 70, 2.0 ** 127])
+@pytest.mark.parametrize("sign", [-1, 1])
+def test_attention_of_equal_and_far_scores(d, fresh, length, magnitude, sign):
+    """Scores up to the largest numbers there are.  Where all of a row's tokens have the same, the output is their values' mean; a token whose key is twice as
+    large (rows 70 on of the second head see it) has all the weight, or none where scores are negative.
+
+    One element of a key is not zero, so that scores are exact.  The weights of equal scores are one and the same number, in all parts of a row: what is left are
+    binary32 sums of `count` values and the join's, (count + 64) 2^-23 of the values' mean magnitude.  The larger key's scores differ by 2^11 and more in units of log2."""
+    big = length - fresh // 2 - 1
+
+    def alter(s, k, v):
+        k[:] = 0
+        k[..., 5] = 1
+        k[big, 1, 5] = 2 if magnitude < 2.0 ** 127 else 1
+    seqs = Sequences(fresh + d, [fresh], [length], d, 2, 32).fill(alter)
+    scale = np.log(2.0) * (1 - 2.0 ** -20)
+    q = np.zeros((fresh, 4, d), dtype=np.float32)
+    q[..., 5] = sign * 1.9921875 * magnitude
+    out = guarded(fresh, 4 * d)
+    arrays = [dev(bs.bits_of(q, mm.BF16).reshape(fresh, -1)), out, dev(seqs.memory), dev(seqs.table), dev(np.array(seqs.lengths, dtype=np.int32)), dev(seqs.begins)]
+    shape = seqs.shape(4)
+    size = mm.attention_fp4_workspace(mm.BF16, max_length=length, **shape)
+    assert (size > 0) == (length > 2000)
+    ws = torch.empty(size + 16, dtype=torch.uint8, device="cuda")
+    mm.attention_fp4(*arrays, ws if size else None, mm.BF16, **shape, max_length=length, scale=float(scale), workspace_bytes=size)
+    torch.cuda.synchronize()
+    got = bs.values_of(out.cpu().numpy().view(np.uint16), mm.BF16).reshape(fresh, 2, 2, d)
+    _, v, _ = oc.read(seqs.memory, seqs.table[0], seqs.page, length, d)
+    for i in range(fresh):
+        seen = length - fresh + i + 1
+        for h in range(2):
+            use = np.arange(seen)
+            if h == 1 and seen > big and magnitude < 2.0 ** 127 and seen > 1:
+                use = use[use == big] if sign > 0 else use[use != big]
+            want, most = v[use, h].mean(0), np.abs(v[use, h]).mean(0)
+            room = (seen + 64) * 2.0 ** -23 * most
+            assert (np.abs(got[i, h] - want) <= room + 2.0 ** -8 * (np.abs(want) + room)).all(), (i, h)
 
 
 def test_attention_past_32_bits_of_bytes():

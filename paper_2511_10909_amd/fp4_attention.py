@@ -30,7 +30,7 @@ class Fp4Cache:
         self._users = [0] * pages
         self._pages, self._lengths = {}, {}
         self._next = 0
-        self.generation = 0                                             # counts the changes that make older batches' tables wrong
+        self.generation = 0                                             # counts the changes after which older batches would read or write others' pages
 
     def __contains__(self, sequence):
         return sequence in self._pages
@@ -52,6 +52,7 @@ class Fp4Cache:
 
     def _copy(self, moves):
         if moves:
+            _is_current(self.device)
             mm.cache_copy_pages(self.memory, torch.tensor(moves, dtype=torch.int32), self.pages, self.page_bytes, self.layers)
 
     def extend(self, sequence, tokens):
@@ -67,8 +68,9 @@ class Fp4Cache:
         if max(fresh, 0) + bool(shared) > len(self._free):
             raise ValueError("%d pages are asked for, %d are free" % (max(fresh, 0) + bool(shared), len(self._free)))
         if shared:
-            page = self._free.pop()
+            page = self._free[-1]
             self._copy([(held[-1], page)])
+            self._free.pop()
             self._users[held[-1]] -= 1
             self._users[page] = 1
             held[-1] = page
@@ -80,11 +82,12 @@ class Fp4Cache:
         self._lengths[sequence] = length + tokens
 
     def fork(self, sequence):
-        """A sequence with the same tokens, in the same pages."""
+        """A sequence with the same tokens, in the same pages.  Batches made before it are not for any further call: they would write into pages that are shared now."""
         other = self.new()
         self._pages[other], self._lengths[other] = list(self._pages[sequence]), self._lengths[sequence]
         for page in self._pages[other]:
             self._users[page] += 1
+        self.generation += 1
         return other
 
     def free(self, sequence):
@@ -130,8 +133,8 @@ class Fp4Cache:
 
 
 class Batch:
-    """What the operators read of a call: page tables, lengths and first rows on the device.  `advance` is the next token of each sequence, as a captured graph
-    may do it; the room for it is taken beforehand (`reserve`)."""
+    """What the operators read of a call: page tables, lengths and first rows on the device.  A captured graph may count `lengths` on by itself, where the room for its
+    replays was taken beforehand (Fp4Cache.extend); a replay is not checked: fork, free and compact wait until it is done, and it is captured anew after them."""
 
     def __init__(self, cache, sequences, counts):
         self.cache, self.sequences, self.generation = cache, sequences, cache.generation
@@ -151,6 +154,11 @@ class Batch:
         c = self.cache
         return dict(dim=c.dim, heads=heads, kv_heads=c.kv_heads, page_tokens=c.page_tokens, pages=c.pages, sequences=len(self.sequences),
                     table_stride=self.table.shape[1], tokens=self.tokens, max_tokens=self.max_tokens)
+
+
+def _is_current(device):
+    if device.type == "cuda" and device.index != torch.cuda.current_device():
+        raise ValueError("the cache is on %s, the current device is cuda:%d" % (device, torch.cuda.current_device()))
 
 
 def rotation_table(positions, rotary_dim, theta=10000.0, device="cuda"):
@@ -185,6 +193,7 @@ class Fp4Attention:
         d, kv, tokens = cache.dim, cache.kv_heads, batch.tokens
         if batch.generation != cache.generation:
             raise ValueError("the batch is older than the last change of the cache's pages")
+        _is_current(cache.device)
         if not 0 <= layer < cache.layers:
             raise ValueError("layer %d of a cache of %d" % (layer, cache.layers))
         if heads <= 0 or heads % kv:

@@ -140,3 +140,40 @@ def test_refusals():
     cache.free(s)
     with pytest.raises(ValueError):
         fa.Fp4Attention(4)(**good)
+
+
+def test_a_batch_older_than_a_fork_is_refused(copies):
+    """It would write into pages that two sequences share by then."""
+    cache = fa.Fp4Cache(1, 4, 1, 64, 32, device="cpu")
+    a = cache.new()
+    batch = cache.batch([a], 5)
+    cache.fork(a)
+    with pytest.raises(ValueError):
+        fa.Fp4Attention(1)(torch.zeros((5, 3 * 64), dtype=torch.bfloat16), batch, 0, torch.zeros((5, 64), dtype=torch.bfloat16))
+
+
+def test_a_copy_that_fails_takes_no_page(monkeypatch):
+    def fail(*a, **kw):
+        raise RuntimeError("no")
+    monkeypatch.setattr(mm, "cache_copy_pages", fail)
+    cache = fa.Fp4Cache(1, 4, 1, 64, 32, device="cpu")
+    a = cache.new()
+    cache.extend(a, 5)
+    b = cache.fork(a)
+    with pytest.raises(RuntimeError):
+        cache.extend(b, 1)
+    assert cache.free_pages() == 3 and cache.pages_of(b) == cache.pages_of(a) and cache.length(b) == 5 and cache._users == [2, 0, 0, 0]
+
+
+def test_work_for_another_device_than_the_current_one_is_refused(copies, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    cache = fa.Fp4Cache(1, 4, 1, 64, 32, device="cpu")
+    a = cache.new()
+    batch = cache.batch([a], 5)
+    cache.device = torch.device("cuda", 1)
+    with pytest.raises(ValueError):
+        fa.Fp4Attention(1)(torch.zeros((5, 3 * 64), dtype=torch.bfloat16), batch, 0, torch.zeros((5, 64), dtype=torch.bfloat16))
+    b = cache.fork(a)
+    with pytest.raises(ValueError):
+        cache.extend(b, 1)
+    assert not copies

@@ -21,7 +21,8 @@ constexpr float LOWEST = -3.4028234663852886e38f;  // a maximum over nothing: no
 // Weights are held times 2^SHIFT, relative to a maximum that moves where those of a granule come to LIMIT together: it may lie 2^11 below.  Weights down to 2^-18
 // of the largest keep FP16's eleven bits, and smaller ones are off by 2^-29 of it at most.
 constexpr float SHIFT = 4.0f, LIMIT = 32768.0f;
-// From here on the rounding of a maximum, which a weight's fused product does not have, is no longer small beside its exponent (a quarter at most below): products are rounded too.
+// A maximum is rounded, the product in a weight's exponent is not (it is fused with the difference).  Below this that is a quarter at most; from here on the weights are those that are
+// made again where maxima move, whose products are rounded as well.
 constexpr float FAR = 4194304.0f;
 
 // The granules that the rows r0 .. of a block see, and the parts that workgroups take of them, `chunk` each.

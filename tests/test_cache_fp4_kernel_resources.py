@@ -1,5 +1,5 @@
 """Registers of the kernels around the cache in 4 bits, checked at compile time (no GPU).  A wavefront of attention holds its rows' queries, sums and two granules: the shapes
-that take single tokens and the long prompts of heads of 128 need no scratch memory, the others a few words; the rest needs none."""
+that take up to three tiles of heads of 128, and single tokens, need no scratch memory, the others a few words; the rest needs none."""
 import os
 import re
 import shutil
@@ -27,6 +27,6 @@ def test_registers_suffice(source, kernel, count):
     for b in blocks:
         get = lambda key: int(re.search(key + r":\s*(\d+)", b).group(1))
         tiles = re.search(r"attention_kernelILi\dELi(\d+)ELi(\d)E", b.split("\n")[0])
-        allowed = 0 if tiles is None or tiles.groups() in (("64", "1"), ("128", "1"), ("128", "3")) else 16
+        allowed = 0 if tiles is None or tiles.groups() in (("64", "1"), ("128", "1"), ("128", "2"), ("128", "3")) else 32
         assert get("VGPRs Spill") <= allowed, b
         assert get(r"Occupancy \[waves/SIMD\]") >= (2 if tiles else 4), b

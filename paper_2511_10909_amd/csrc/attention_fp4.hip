@@ -91,11 +91,11 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
     // this lane's rows: query operands, and positions (rows that are not there: the last one again)
     Frag16 q[Q_LDS ? 1 : NR][J];
     u32x4 *const wave_q = lds_q + (ROW_WAVES > 1 ? wave * (NR * J * 64) : 0) + lane;
-    int32_t pos[NR];
+    uint32_t apart = 0;                            // bytes: how far a tile's row lies behind the wavefront's first position (less than 64 tokens)
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         const uint32_t r = r0 + 16 * i + l < rows ? r0 + 16 * i + l : rows - 1, token = r / a.group, h = r % a.group;
-        pos[i] = sq.start + (int32_t)token;
+        apart |= (token - r0 / a.group & 0xFFu) << (8 * i);
         if (Q_LDS && ROW_WAVES == 1 && (uint32_t)i % WAVES != wave) continue;      // (the same for all wavefronts: they share them)
         const uint16_t *at = (const uint16_t *)a.q + (uint64_t)(sq.first + token) * a.q_stride + (uint64_t)(head * a.group + h) * D + g * (D / 4);
 #pragma unroll
@@ -148,16 +148,20 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
         const int32_t t0 = (int32_t)(32 * (from + skip + n * TOKEN_WAVES));
         // whether all rows see all of the granule
         const bool whole = t0 + 31 <= pos_first && (!a.window || (uint32_t)(pos_last - t0) < a.window);
-        const auto sees = [&](int32_t t, int i) { return t <= pos[i] && (!a.window || (uint32_t)(pos[i] - t) < a.window); };
-        // the lane's first token, for branches that few granules take: its value is hidden, or what is made of it would be made for all
-        const auto first_token = [&]() {
-            int32_t t = t0 + 8 * (int32_t)g;
-            asm volatile("" : "+v"(t));
-            return t;
+        // the lane's first token and its rows' distances, for branches that few granules take: their values are hidden, or what is made of them would be made for all
+        struct Mask { int32_t t; uint32_t apart; };
+        const auto mask = [&]() {
+            Mask x = {t0 + 8 * (int32_t)g, apart};
+            asm volatile("" : "+v"(x.t), "+v"(x.apart));
+            return x;
+        };
+        const auto sees = [&](const Mask &x, int e, int i) {
+            const int32_t behind = pos_first + (int32_t)(x.apart >> (8 * i) & 0xFFu) - (x.t + e);
+            return behind >= 0 && (!a.window || (uint32_t)behind < a.window);
         };
         if (!whole) {
             // tokens that no row sees may hold anything: their V scales become the least
-            const int32_t t = first_token();
+            const int32_t t = mask().t;
             const int32_t low = a.window && (uint32_t)(pos_first < 0 ? 0 : pos_first) >= a.window ? pos_first + 1 - (int32_t)a.window : 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -181,11 +185,11 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
         }
         load_keys<D>(xk, at, off);
         if (!whole) {
-            const int32_t t = first_token();
+            const Mask x = mask();
 #pragma unroll
             for (int i = 0; i < NR; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sc[i][e / 4][e % 4] = sees(t + e, i) ? sc[i][e / 4][e % 4] : -__builtin_inff();
+                for (int e = 0; e < 8; ++e) sc[i][e / 4][e % 4] = sees(x, e, i) ? sc[i][e / 4][e % 4] : -__builtin_inff();
         }
         // Weights against the maximum as it was, and their sums over the granule, which the matrix instruction makes as well.  Where a tile's sum comes to LIMIT (or is
         // NaN, or a weight has left FP16), its maxima move and its weights are made again.
@@ -237,7 +241,7 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
         for (int i = 0; i < NR; ++i) sum[i] += add[i];
         // NaN blocks among the values: they are taken as zeros, and make NaN the outputs of the rows that see them
         if (__any(any_nan_code(xv.scales[0]) | any_nan_code(xv.scales[1]))) {
-            const int32_t t = first_token();
+            const Mask x = mask();
             f16x8 bad;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -249,7 +253,7 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
             for (int i = 0; i < NR; ++i) {
                 f16x8 seen;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) seen[e] = sees(t + e, i) ? (_Float16)1.0f : (_Float16)0.0f;
+                for (int e = 0; e < 8; ++e) seen[e] = sees(x, e, i) ? (_Float16)1.0f : (_Float16)0.0f;
                 const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad, seen, f32x4{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
                 for (uint32_t d = 0; d < DT; ++d)
@@ -415,10 +419,10 @@ struct Plan { uint32_t nr, row_waves, waves, block_rows, blocks, splits, chunk; 
 // or four times, none below four granules a wavefront: 64 sequences of up to 16384 tokens 173 us in one part, 147 in two, 152 in eight; one of 131072 47 us in 16 parts, 31 in 32.
 //
 // More rows: four wavefronts of `nr` tiles each.  The more tiles, the fewer conversions a row costs, but the fewer workgroups there are: the choice goes by the granules that all
-// workgroups of three tiles would see, us with one, two and three tiles: 1500 tokens x 32 heads (6000 granules) 43, 50 and 58; 3000 (24000) 115, 109 and 112; 500 over 8000
-// (21000) 122, 104 and 117; 8192 (176000) 585 with two, 543 with three.  Parts where a row sees much more than comes with the call, or the blocks' order, longest first, would not even
+// workgroups of three tiles would see, us with one, two and three tiles: 1500 tokens x 32 heads (6000 granules) 43, 48 and 58; 2500 (17000) 89, 80 and 94; 3000 (24000) 115, 106
+// and 114; 500 over 8000 (22000) 137, 102 and 110; 4000 (42000) 188, 172 and 157; 8192 (175000) 725, 606 and 540.  Parts where a row sees much more than comes with the call, or the blocks' order, longest first, would not even
 // them out: so that few blocks fill the chip once (100 tokens over 8000: 180 us in one part, 44 in eight; 500: 222 and 104 in four), and many are cut
-// small enough, but not below 24 granules (six sequences of up to 1030 over 6007: 410 us in one part, 378 in three; four of up to 500 over 2500: 93 in two, 111 in six).  A prompt by itself takes 543 us in one part and 646 in two.
+// small enough, but not below 24 granules (six sequences of up to 1030 over 6007: 410 us in one part, 378 in three; four of up to 500 over 2500: 93 in two, 111 in six).  A prompt by itself takes 540 us in one part and 646 in two.
 static Plan plan_of(const mmaemu_attention_fp4_args &a)
 {
     const uint32_t group = a.heads / a.kv_heads, rows = a.max_tokens * group;
@@ -436,7 +440,7 @@ static Plan plan_of(const mmaemu_attention_fp4_args &a)
     } else {
         p.row_waves = p.waves = 4;
         const uint64_t triples = heads * ((rows + 191) / 192), all = triples * (seen >= 2ull * a.max_tokens ? granules : (granules + 1) / 2);
-        p.nr = all <= 20000 ? 1 : all <= 40000 ? 2 : 3;
+        p.nr = all <= 10000 ? 1 : all <= 40000 ? 2 : 3;
         p.blocks = (rows + 64 * p.nr - 1) / (64 * p.nr);
         const uint64_t groups = heads * p.blocks;
         splits = seen < 2ull * a.max_tokens || !groups ? 1 : groups <= 256 ? 512 / groups : (2600 + groups - 1) / groups;

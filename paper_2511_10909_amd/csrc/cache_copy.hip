@@ -7,17 +7,18 @@
 namespace mmaemu {
 
 constexpr uint32_t COPY_MOVES = 440;               // of a launch: 8 bytes each within the 4 KB that a launch's arguments may take
+constexpr uint32_t COPY_FEW = 32;                  // most calls' moves: FEW_US
 constexpr uint32_t COPY_STRETCH = 16384;           // bytes of a workgroup
 
-struct CopyArgs {
+template <uint32_t MOVES> struct CopyArgs {
     uint8_t *memory;
     uint64_t page_bytes, layer_bytes;
     uint32_t stretches;                            // of a page
     uint32_t reserved;
-    int32_t moves[2 * COPY_MOVES];
+    int32_t moves[2 * MOVES];
 };
 
-__global__ void __launch_bounds__(256) cache_copy_kernel(const CopyArgs a)
+template <uint32_t MOVES> __global__ void __launch_bounds__(256) cache_copy_kernel(const CopyArgs<MOVES> a)
 {
     const uint32_t move = blockIdx.x / a.stretches, stretch = blockIdx.x % a.stretches;
     uint8_t *const layer = a.memory + blockIdx.y * a.layer_bytes;
@@ -38,9 +39,9 @@ __global__ void __launch_bounds__(256) cache_copy_kernel(const CopyArgs a)
     }
 }
 
-mmaemu_status launch_cache_copy(void *memory, const int32_t *moves, uint64_t count, uint64_t page_bytes, uint64_t layers, uint64_t layer_bytes, hipStream_t s)
+template <uint32_t MOVES> static mmaemu_status launch_moves(void *memory, const int32_t *moves, uint64_t count, uint64_t page_bytes, uint64_t layers, uint64_t layer_bytes, hipStream_t s)
 {
-    CopyArgs a;
+    CopyArgs<MOVES> a;
     a.memory = (uint8_t *)memory;
     a.page_bytes = page_bytes;
     a.layer_bytes = layer_bytes;
@@ -50,17 +51,23 @@ mmaemu_status launch_cache_copy(void *memory, const int32_t *moves, uint64_t cou
         // (moves of a page onto itself are left out; a launch's threads count in 32 bits)
         const uint64_t most = (1u << 23) / a.stretches;
         uint32_t n = 0;
-        for (; m < count && n < COPY_MOVES && n < (most ? most : 1); ++m) {
+        for (; m < count && n < MOVES && n < (most ? most : 1); ++m) {
             if (moves[2 * m] == moves[2 * m + 1]) continue;
             a.moves[2 * n] = moves[2 * m];
             a.moves[2 * n + 1] = moves[2 * m + 1];
             ++n;
         }
         if (!n) break;
-        hipLaunchKernelGGL(cache_copy_kernel, dim3(n * a.stretches, (uint32_t)layers), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(cache_copy_kernel<MOVES>, dim3(n * a.stretches, (uint32_t)layers), dim3(256), 0, s, a);
         MMAEMU_HIP(hipGetLastError());
     }
     return MMAEMU_OK;
+}
+
+mmaemu_status launch_cache_copy(void *memory, const int32_t *moves, uint64_t count, uint64_t page_bytes, uint64_t layers, uint64_t layer_bytes, hipStream_t s)
+{
+    if (count <= COPY_FEW) return launch_moves<COPY_FEW>(memory, moves, count, page_bytes, layers, layer_bytes, s);
+    return launch_moves<COPY_MOVES>(memory, moves, count, page_bytes, layers, layer_bytes, s);
 }
 
 } // namespace mmaemu

@@ -56,6 +56,21 @@ template <int T, int D, int A> __device__ __forceinline__ Frag16 k_operand(const
     return T == MMAEMU_BF16 ? keys_bf16(word, scale_of<A>(x.scales)) : keys_fp16(word, scale_of<A>(x.scales));
 }
 
+// The sequence of rank k by length, the longest first (up to 64 of them; equal ones in order).  Workgroups start in the order of their indexes, and where few of them fill
+// the chip, the last to start should have the least to do: six chunks of 391 to 1030 tokens over 2159 to 6007 take 323 us in
+// that order, 410 in the call's.
+__device__ __forceinline__ uint32_t by_length(const CacheArgs &c, uint32_t k)
+{
+    const uint32_t lane = threadIdx.x & 63u;
+    const int32_t length = lane < c.sequences ? c.lengths[lane] : 0;
+    uint32_t rank = 0;
+    for (uint32_t j = 0; j < c.sequences; ++j) {
+        const int32_t other = __builtin_amdgcn_readlane(length, (int)j);
+        rank += other > length || (other == length && j < lane);
+    }
+    return (uint32_t)__builtin_ctzll(__ballot(lane < c.sequences && rank == k));
+}
+
 // Rows of NR x 16 x ROW_WAVES, tokens split over the other wavefronts.  Where the tiles of rows are many, the queries wait in LDS.  As many wavefronts a SIMD as registers
 // allow without scratch memory in the loop: two tiles of heads of 128 at three 134 us, at two 108 (3000 tokens x 32 heads); three tiles of heads of 64 at two 386 us,
 // at three, with five words of scratch, 350 (8192 tokens x 32 heads).
@@ -69,7 +84,7 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
     __shared__ u32x4 lds_q[Q_LDS ? ROW_WAVES * NR * J * 64 : 1];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15u;
     const uint32_t head = blockIdx.x % a.c.kv_heads, block = a.blocks - 1 - blockIdx.x / a.c.kv_heads;        // the longest rows first
-    const uint32_t split = blockIdx.y, s = blockIdx.z;
+    const uint32_t split = blockIdx.y, s = ROW_WAVES > 1 && a.c.sequences > 1 && a.c.sequences <= 64 ? by_length(a.c, blockIdx.z) : blockIdx.z;
     const Sequence sq = sequence_of(a.c, s);
     const uint32_t rows = (sq.n < a.max_tokens ? sq.n : a.max_tokens) * a.group;
     if (block * ROWS >= rows) return;
@@ -420,9 +435,11 @@ struct Plan { uint32_t nr, row_waves, waves, block_rows, blocks, splits, chunk; 
 //
 // More rows: four wavefronts of `nr` tiles each.  The more tiles, the fewer conversions a row costs, but the fewer workgroups there are: the choice goes by the granules that all
 // workgroups of three tiles would see, us with one, two and three tiles: 1500 tokens x 32 heads (6000 granules) 43, 48 and 58; 2500 (17000) 89, 80 and 94; 3000 (24000) 115, 106
-// and 114; 500 over 8000 (22000) 137, 102 and 110; 4000 (42000) 188, 172 and 157; 8192 (175000) 725, 606 and 540.  Parts where a row sees much more than comes with the call, or the blocks' order, longest first, would not even
-// them out: so that few blocks fill the chip once (100 tokens over 8000: 180 us in one part, 44 in eight; 500: 222 and 104 in four), and many are cut
-// small enough, but not below 24 granules (six sequences of up to 1030 over 6007: 410 us in one part, 378 in three; four of up to 500 over 2500: 93 in two, 111 in six).  A prompt by itself takes 540 us in one part and 646 in two.
+// and 114; 500 over 8000 (22000) 137, 102 and 110; 4000 (42000) 188, 172 and 157; 8192 (175000) 725, 606 and 540.
+// Parts where a row sees much more than comes with the call and workgroups are few: so that they fill the chip once (100 tokens over 8000: 178 us in one part, 42 in nine; 500: 217
+// and 103 in four), twice (700 over 8000: 218 in one, 172 in two, 154 in five; 1500 over 12000: 388, 328, and 321 in four) or nearly three times (2048 over 16384: 743 in one, 595 in
+// four).  From 450 on the order, longest first, evens them out, and joining the parts costs more than they bring: six chunks of 391 to 1030 tokens over 2159 to
+// 6007 323 us in one part, 380 in three; six of 1030 over 6007 644 and 706; 3000 tokens over 9000 399 and 426.
 static Plan plan_of(const mmaemu_attention_fp4_args &a)
 {
     const uint32_t group = a.heads / a.kv_heads, rows = a.max_tokens * group;
@@ -443,8 +460,8 @@ static Plan plan_of(const mmaemu_attention_fp4_args &a)
         p.nr = all <= 10000 ? 1 : all <= 40000 ? 2 : 3;
         p.blocks = (rows + 64 * p.nr - 1) / (64 * p.nr);
         const uint64_t groups = heads * p.blocks;
-        splits = seen < 2ull * a.max_tokens || !groups ? 1 : groups <= 256 ? 512 / groups : (2600 + groups - 1) / groups;
-        least = groups <= 256 ? 4 : 24;
+        splits = seen < 2ull * a.max_tokens || !groups || groups >= 450 ? 1 : (groups <= 128 ? 512 : groups <= 256 ? 1050 : 1400) / groups;
+        least = groups <= 128 ? 4 : groups <= 256 ? 8 : 32;
     }
     p.block_rows = 16 * p.nr * p.row_waves;
     if (splits > granules / least) splits = granules / least;

@@ -251,22 +251,37 @@ def test_attention_over_long_caches(d, fresh, length, window):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("empty", [290, 650])
+@pytest.mark.parametrize("empty", [105, 215])
 @pytest.mark.parametrize("window", [0, 40, 1300])
 def test_attention_of_chunks_among_many_sequences(d, empty, window):
     """Chunks over long caches in a batch whose other sequences bring nothing: wavefronts of two and three tiles of rows, in one part and in two."""
     def alter(s, k, v):
         if s == 1:
             v[3, 0], k[9, 1, 3], v[-1, 1, :32] = np.nan, np.nan, np.inf
-    fresh, lengths = [48, 45, 17, 1, 48] + [0] * empty, [1536, 800, 1500, 900, 1530] + [0] * empty
+    fresh, lengths = [48, 45, 17, 1, 48] + [0] * empty, [3000, 800, 1500, 900, 2530] + [0] * empty
     seqs = Sequences(empty, fresh, lengths, d, 2, 64).fill(alter)
     seqs.table[4, 1] = -1
     shape = seqs.shape(8)
     # (two parts; the plan counts a window's tokens where they are fewer)
-    size = mm.attention_fp4_workspace(mm.BF16, max_length=1536, window=window, **shape)
+    size = mm.attention_fp4_workspace(mm.BF16, max_length=3000, window=window, **shape)
     assert size == (2 * seqs.tokens * 8 * (d + 2) * 4 if window == 0 else 0)
     run_attention(seqs, 8, mm.BF16, window=window, pad=8)
     run_attention(seqs, 8, mm.FP16, window=window, in_place=True, max_length=100000)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sequences", [2, 63, 64, 65])
+def test_attention_in_any_order_of_lengths(d, sequences):
+    """The longest sequences' workgroups start first: equal lengths, sequences that bring nothing, lengths that are none."""
+    rng = np.random.default_rng(sequences)
+    fresh = [int(x) for x in rng.integers(0, 25, sequences)]
+    fresh[0], fresh[-1] = 25, 20
+    lengths = [f + 40 * int(x) for f, x in zip(fresh, rng.integers(0, 4, sequences))]
+    # (a sequence whose length will say more than was written has its pages full: what other bytes mean as scales is nowhere said)
+    lengths[sequences // 3] = -(-max(lengths[sequences // 3], 1) // 32) * 32
+    seqs = Sequences(sequences, fresh, lengths, d, 1, 32).fill()
+    seqs.lengths[sequences // 2], seqs.lengths[sequences // 3] = -5, 10 ** 6
+    run_attention(seqs, 3, mm.FP16, max_length=300)
 
 
 @pytest.mark.parametrize("d", [64, 128])

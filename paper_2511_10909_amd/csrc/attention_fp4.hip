@@ -58,7 +58,7 @@ template <int T, int D, int A> __device__ __forceinline__ Frag16 k_operand(const
 
 // The sequence of rank k by length, the longest first (up to 64 of them; equal ones in order).  Workgroups start in the order of their indexes, and where few of them fill
 // the chip, the last to start should have the least to do: six chunks of 391 to 1030 tokens over 2159 to 6007 take 323 us in
-// that order, 410 in the call's.
+// that order, 406 in the call's.  (Prompts by themselves are not put in order: their own workgroups see from nothing to all; four of up to 4000 tokens 390 us, 371 without.)
 __device__ __forceinline__ uint32_t by_length(const CacheArgs &c, uint32_t k)
 {
     const uint32_t lane = threadIdx.x & 63u;
@@ -84,7 +84,7 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
     __shared__ u32x4 lds_q[Q_LDS ? ROW_WAVES * NR * J * 64 : 1];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15u;
     const uint32_t head = blockIdx.x % a.c.kv_heads, block = a.blocks - 1 - blockIdx.x / a.c.kv_heads;        // the longest rows first
-    const uint32_t split = blockIdx.y, s = ROW_WAVES > 1 && a.c.sequences > 1 && a.c.sequences <= 64 ? by_length(a.c, blockIdx.z) : blockIdx.z;
+    const uint32_t split = blockIdx.y, s = ROW_WAVES > 1 && a.ordered ? by_length(a.c, blockIdx.z) : blockIdx.z;
     const Sequence sq = sequence_of(a.c, s);
     const uint32_t rows = (sq.n < a.max_tokens ? sq.n : a.max_tokens) * a.group;
     if (block * ROWS >= rows) return;
@@ -427,7 +427,7 @@ template <int T, int D, uint32_t AT_ONCE> __global__ void __launch_bounds__(256)
 }
 
 // ---- which shape, and how many parts ---------------------------------------------------------
-struct Plan { uint32_t nr, row_waves, waves, block_rows, blocks, splits, chunk; };
+struct Plan { uint32_t nr, row_waves, waves, block_rows, blocks, splits, chunk; bool ordered; };
 
 // Up to 64 rows of a KV head (a token's, a few drafts'): one workgroup has them all, its wavefronts share the tokens.  Eight wavefronts where workgroups are few (one
 // sequence, 513 tokens: 6.5 us, 7.5 with four; 131072 tokens: 31 and 33), four else (24 sequences of 35 rows: 21 and 23).  Parts: as many as fill the chip once (eight wavefronts)
@@ -446,6 +446,7 @@ static Plan plan_of(const mmaemu_attention_fp4_args &a)
     const uint64_t seen = a.window && (uint64_t)a.window + a.max_tokens < a.max_length ? (uint64_t)a.window + a.max_tokens : a.max_length;
     const uint64_t granules = (seen + 31) / 32, heads = (uint64_t)a.kv_heads * a.sequences;
     Plan p;
+    p.ordered = false;
     uint64_t splits, least;
     if (rows <= 64) {
         p.row_waves = 1;
@@ -462,6 +463,7 @@ static Plan plan_of(const mmaemu_attention_fp4_args &a)
         const uint64_t groups = heads * p.blocks;
         splits = seen < 2ull * a.max_tokens || !groups || groups >= 450 ? 1 : (groups <= 128 ? 512 : groups <= 256 ? 1050 : 1400) / groups;
         least = groups <= 128 ? 4 : groups <= 256 ? 8 : 32;
+        p.ordered = a.sequences > 1 && a.sequences <= 64 && seen >= 2ull * a.max_tokens;
     }
     p.block_rows = 16 * p.nr * p.row_waves;
     if (splits > granules / least) splits = granules / least;
@@ -514,6 +516,7 @@ mmaemu_status launch_attention_fp4(const mmaemu_attention_fp4_args &a, const Cac
     const Plan plan = plan_of(a);
     AttentionArgs p = {c, a.q, a.out, (float *)a.workspace, nullptr, a.q_stride, a.out_stride, a.heads, a.heads / a.kv_heads, a.max_tokens, a.window, plan.blocks,
                        plan.splits, plan.chunk, (float)(a.scale * 1.4426950408889634)};
+    p.ordered = plan.ordered;
     p.stat = (f32x2 *)(p.part + (uint64_t)plan.splits * a.tokens * a.heads * a.dim);
     if (a.type == MMAEMU_BF16) return a.dim == 128 ? launch_typed<MMAEMU_BF16, 128>(p, plan, s) : launch_typed<MMAEMU_BF16, 64>(p, plan, s);
     return a.dim == 128 ? launch_typed<MMAEMU_FP16, 128>(p, plan, s) : launch_typed<MMAEMU_FP16, 64>(p, plan, s);

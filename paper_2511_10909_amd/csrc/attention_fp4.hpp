@@ -15,6 +15,7 @@ struct AttentionArgs {
     uint32_t heads, group, max_tokens, window, blocks;                 // blocks: of rows, of a sequence's KV head
     uint32_t splits, chunk;                        // most workgroups that share a row's granules, and how many granules make one more worth it
     float c2;                                      // scale log2(e)
+    uint32_t ordered;                              // whether sequences are taken by their lengths
 };
 
 constexpr float LOWEST = -3.4028234663852886e38f;  // a maximum over nothing: no finite score lies below it

@@ -282,6 +282,7 @@ def test_attention_in_any_order_of_lengths(d, sequences):
     seqs = Sequences(sequences, fresh, lengths, d, 1, 32).fill()
     seqs.lengths[sequences // 2], seqs.lengths[sequences // 3] = -5, 10 ** 6
     run_attention(seqs, 3, mm.FP16, max_length=300)
+    run_attention(seqs, 3, mm.BF16, max_length=1)
 
 
 @pytest.mark.parametrize("d", [64, 128])

@@ -5,6 +5,9 @@
 //   s = scale log2(e) q.k;  m' = max(m, max s);  p = 2^(s - m');  l = l 2^(m - m') + sum p;  O = O 2^(m - m') + p V;  out = O / l
 // Both products are 16 x 16 x 32 instructions on operands that lie in the cache as the lanes take them (cache_fp4.hpp), brought to 16 bits, which is
 // exact: K to the queries' type, V to FP16.  The scores' registers are the second product's operand as they are, rounded to FP16.
+//
+// Few rows are bound by memory: 64 sequences of up to 16384 tokens, 64 heads over 8 of 128, 147 us, 4.9 TB/s.  Prompts are bound by the SIMDs' issue port, which matrix
+// instructions hold for ten cycles, exponentials for eight and other vector instructions for four: 8192 tokens x 32 heads 541 us, 1.0 PFLOP/s of the products that are needed.
 #include "attention_fp4.hpp"
 
 namespace mmaemu {

@@ -434,7 +434,9 @@ struct Plan { uint32_t nr, row_waves, waves, block_rows, blocks, splits, chunk; 
 
 // Up to 64 rows of a KV head (a token's, a few drafts'): one workgroup has them all, its wavefronts share the tokens.  Eight wavefronts where workgroups are few (one
 // sequence, 513 tokens: 6.5 us, 7.5 with four; 131072 tokens: 31 and 33), four else (24 sequences of 35 rows: 21 and 23).  Parts: as many as fill the chip once (eight wavefronts)
-// or four times, none below four granules a wavefront: 64 sequences of up to 16384 tokens 173 us in one part, 147 in two, 152 in eight; one of 131072 47 us in 16 parts, 31 in 32.
+// or are resident at once (four; registers leave half as many with two tiles and more of heads of 128), none below four granules a wavefront: 64 sequences of up to 16384 tokens 173 us
+// in one part, 147 in two, 152 in eight; one of 131072 47 us in 16 parts, 31 in 32; eight sequences of 64 rows over 8000 41 us in eight parts, 55 in fifteen; 32 of 32 rows over up to
+// 4000 35 in two, 40 in four.
 //
 // More rows: four wavefronts of `nr` tiles each.  The more tiles, the fewer conversions a row costs, but the fewer workgroups there are: the choice goes by the granules that all
 // workgroups of three tiles would see, us with one, two and three tiles: 1500 tokens x 32 heads (6000 granules) 43, 48 and 58; 2500 (17000) 89, 80 and 94; 3000 (24000) 115, 106
@@ -456,7 +458,7 @@ static Plan plan_of(const mmaemu_attention_fp4_args &a)
         p.nr = (rows + 15) / 16;
         p.blocks = 1;
         p.waves = heads <= 32 ? 8 : 4;
-        splits = heads ? (p.waves == 8 ? 256 : 1024) / heads : 1;
+        splits = heads ? (p.waves == 8 ? 256 : a.dim == 128 && p.nr > 1 ? 512 : 1024) / heads : 1;
         least = 4 * p.waves;
     } else {
         p.row_waves = p.waves = 4;

@@ -374,7 +374,7 @@ def run(s):
                             q_stride=stride, k_stride=stride, v_stride=stride, k_values=s["k_values"], v_values=s["v_values"])
         return dict(q=s["q_out"], k=s["k_values"], v=s["v_values"], cache=s["cache"])
     if s["workspace"] is None:                       # as a program keeps it for all its calls
-        size = mm.attention_fp4_workspace(t, max_length=s["longest"], **shape)
+        size = mm.attention_fp4_workspace(t, max_length=s["longest"], window=case["window"], **shape)
         s["workspace"] = torch.empty(max(size, 16), dtype=torch.uint8, device="cuda")
     mm.attention_fp4(s["q"], s["out"], s["cache"], s["table"], s["lengths"], s["begins"], s["workspace"], t, max_length=s["longest"],
                      window=case["window"], scale=1.0 / math.sqrt(case["dim"]), workspace_bytes=s["workspace"].numel(), **shape)

@@ -686,7 +686,7 @@ mmaemu_status mmaemu_cache_append_fp4(const mmaemu_cache_append_fp4_args *args);
  *   out[r][h] = sum over t of p_t v_t,  p = softmax over t of scale * (q[r][h] . k_t),  k and v of head h / (heads / kv_heads),
  * over the tokens t <= position of row r, and > position - window where window is not 0.  A row that sees no token gives zeros.  Tokens that a row does not
  * see have no part in it, whatever they hold.
- * Scores, maxima and sums are binary32; the weights p, relative to a maximum that may lie 2^11 below the largest, are rounded to FP16 (nearest even) for the
+ * Scores, maxima and sums are binary32; equal scores of a row have equal weights, whatever their size; the weights p, relative to a maximum that may lie 2^11 below the largest, are rounded to FP16 (nearest even) for the
  * second product: those below 2^-18 of the row's largest are off by up to 2^-29 of it.  A score that leaves binary32 is an infinity: tokens of minus infinity
  * weigh nothing, a row with one of plus infinity is NaN.
  * max_length: the host's bound for lengths; it decides, with the other sizes, over how many workgroups a row's tokens are split, and nothing

@@ -1,8 +1,8 @@
 // Attention over the cache in 4 bits: out = softmax(scale q K^T) V over the tokens that a row sees, from one token to prompts.
 //
 // The rows of a KV head are its group's query heads of all the call's tokens of a sequence, r = token * group + head: they share K and V.  One pass
-// over the tokens with a running maximum m and sum l per row, in units of log2:
-//   s = scale log2(e) q.k;  m' = max(m, max s);  p = 2^(s - m');  l = l 2^(m - m') + sum p;  O = O 2^(m - m') + p V;  out = O / l
+// over the tokens with a running maximum m and sum l per row, c = scale log2(e):
+//   s = q.k;  m' = max(m, max s);  p = 2^(c (s - m'));  l = l 2^(c (m - m')) + sum p;  O = O 2^(c (m - m')) + p V;  out = O / l
 // Both products are 16 x 16 x 32 instructions on operands that lie in the cache as the lanes take them (cache_fp4.hpp), brought to 16 bits, which is
 // exact: K to the queries' type, V to FP16.  The scores' registers are the second product's operand as they are, rounded to FP16.
 //
@@ -141,7 +141,7 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
     // The next granule's keys are read once this one's are used, its values once this one's are: they are on their way during the other's products.
     // (Where a page is none, and past the end, the first granule of the memory is read: a load that always happens costs no branch.)
     bool there = false;
-    float c2 = a.c2;                               // NaN once a maximum has come to FAR, so that all weights are made again (a flag beside it: 559 us, 541 without, 8192 tokens x 32 heads)
+    float c2 = a.c2;                               // NaN once a maximum is far, so that all weights are made again (a flag beside it: 559 us, 541 without, 8192 tokens x 32 heads)
     const uint8_t *at = walk.base;
     const auto advance = [&](uint32_t n) MMAEMU_INLINE {
         if ((n & 63u) == 0 && n && n < mine) walk.refill(n, mine - n);
@@ -216,7 +216,7 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
         f32x4 total[NR];
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const float off = SHIFT - m[i];
+            const float off = reference(m[i], a.c2);
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
                 const f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e / 4][e % 4], c2, off)),
@@ -237,19 +237,18 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
                 if (!__any(!(add[i] < LIMIT))) continue;
                 float top = fmaxf(fmaxf(sc[i][0][0], sc[i][0][1]), fmaxf(sc[i][0][2], sc[i][0][3]));
                 top = fmaxf(top, fmaxf(fmaxf(sc[i][1][0], sc[i][1][1]), fmaxf(sc[i][1][2], sc[i][1][3])));
-                top = fmaxf(m[i], other_rows_max(top) * a.c2);
-                const float factor = __builtin_amdgcn_exp2f(m[i] - top);
+                top = fmaxf(m[i], other_rows_max(top));
+                // from one reference to the other: what both make of the new maximum's own weight
+                const Exponent before(m[i], a.c2), now(top, a.c2);
+                const float factor = __builtin_amdgcn_exp2f(now(top) - before(top));
                 m[i] = top;
                 sum[i] *= factor;
 #pragma unroll
                 for (uint32_t d = 0; d < DT; ++d) acc[i][d] *= factor;
-                if (__any(fabsf(top) >= FAR && top != LOWEST)) c2 = __builtin_nanf("");
-                // (each product rounded as the maximum's was)
+                if (__any(is_far(top, a.c2) && top != LOWEST)) c2 = __builtin_nanf("");
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-#pragma clang fp contract(off)
-                    const float x0 = sc[i][e / 4][e % 4] * a.c2, x1 = sc[i][e / 4][e % 4 + 1] * a.c2;
-                    const f32x2 y = {__builtin_amdgcn_exp2f(x0 - top + SHIFT), __builtin_amdgcn_exp2f(x1 - top + SHIFT)};
+                    const f32x2 y = {__builtin_amdgcn_exp2f(now(sc[i][e / 4][e % 4])), __builtin_amdgcn_exp2f(now(sc[i][e / 4][e % 4 + 1]))};
                     p[i].w[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
                 }
                 add[i] = mfma_fp16(ones, p[i], f32x4{0, 0, 0, 0})[0];
@@ -322,16 +321,23 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
                     }
             } else {
                 const uint64_t row = ((uint64_t)split * a.c.tokens + token) * a.heads + h;
-                if (g == 0) a.stat[row] = f32x2{m[i], sum[i]};
+                const float own = own_factor(m[i], a.c2);
+                if (g == 0) a.stat[row] = f32x2{m[i], sum[i] * own};
                 float *const to = a.part + row * D + 4 * g * DT;
 #pragma unroll
                 for (uint32_t e = 0; e < 4; ++e)
 #pragma unroll
-                    for (uint32_t d = 0; d < DT; d += 4) *reinterpret_cast<f32x4 *>(to + e * DT + d) = f32x4{acc[i][d][e], acc[i][d + 1][e], acc[i][d + 2][e], acc[i][d + 3][e]};
+                    for (uint32_t d = 0; d < DT; d += 4) *reinterpret_cast<f32x4 *>(to + e * DT + d) = f32x4{acc[i][d][e] * own, acc[i][d + 1][e] * own, acc[i][d + 2][e] * own, acc[i][d + 3][e] * own};
             }
         }
     } else {
         // the wavefronts' parts of the same rows meet in LDS, a tile after the other: rows are D + 4 numbers apart
+        float own[NR];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            own[i] = own_factor(m[i], a.c2);
+            sum[i] *= own[i];
+        }
 #pragma unroll
         for (int i = 0; i < NR; ++i)
             if (g == 0) lds_stat[wave * 16 * NR + 16 * i + l] = f32x2{m[i], sum[i]};
@@ -342,7 +348,7 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
             float top = LOWEST;
 #pragma unroll
             for (uint32_t w = 0; w < TOKEN_WAVES; ++w) top = fmaxf(top, lds_stat[w * 16 * NR + 16 * i + l][0]);
-            const float factor = __builtin_amdgcn_exp2f(m[i] - top);
+            const float factor = own[i] * __builtin_amdgcn_exp2f((m[i] - top) * a.c2);
             float *const part = lds + (wave * 16 + l) * (D + 4);
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e)
@@ -361,7 +367,7 @@ template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __laun
 #pragma unroll
                 for (uint32_t w = 0; w < TOKEN_WAVES; ++w) {
                     const f32x2 st = lds_stat[w * 16 * NR + 16 * i + in];
-                    total += st[1] * __builtin_amdgcn_exp2f(st[0] - most);
+                    total += st[1] * __builtin_amdgcn_exp2f((st[0] - most) * a.c2);
                     o += *reinterpret_cast<const f32x4 *>(lds + (w * 16 + in) * (D + 4) + at);
                 }
                 const uint64_t token = sq.first + r / a.group, h = head * a.group + r % a.group;
@@ -410,7 +416,7 @@ template <int T, int D, uint32_t AT_ONCE> __global__ void __launch_bounds__(256)
             top = st[0];
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-            factor = __builtin_amdgcn_exp2f(st[0] - top);
+            factor = __builtin_amdgcn_exp2f((st[0] - top) * a.c2);
         }
 #pragma unroll
         for (uint32_t z = 0; z < AT_ONCE; ++z) {

@@ -10,7 +10,7 @@ struct AttentionArgs {
     const void *q;
     void *out;
     float *part;                                   // [split][token][head][D], unnormalised, and behind them
-    f32x2 *stat;                                   // [split][token][head] (m, l)
+    f32x2 *stat;                                   // [split][token][head]: largest score m, and l, weights relative to 2^(c2 m)
     uint64_t q_stride, out_stride;
     uint32_t heads, group, max_tokens, window, blocks;                 // blocks: of rows, of a sequence's KV head
     uint32_t splits, chunk;                        // most workgroups that share a row's granules, and how many granules make one more worth it
@@ -22,9 +22,20 @@ constexpr float LOWEST = -3.4028234663852886e38f;  // a maximum over nothing: no
 // Weights are held times 2^SHIFT, relative to a maximum that moves where those of a granule come to LIMIT together: it may lie 2^11 below.  Weights down to 2^-18
 // of the largest keep FP16's eleven bits, and smaller ones are off by 2^-29 of it at most.
 constexpr float SHIFT = 4.0f, LIMIT = 32768.0f;
-// A maximum is rounded, the product in a weight's exponent is not (it is fused with the difference).  Below this that is a quarter at most; from here on the weights are those that are
-// made again where maxima move, whose products are rounded as well.
+// A row's weights are 2^(c2 s + reference), and the maximum m of its scores so far decides the reference: -c2 m + SHIFT, rounded.  The product c2 s is fused with the sum, so equal scores
+// have equal weights in all of a row's granules, and what the reference's rounding adds to the exponent, a quarter at most, is the same for all of them.  Where |c2 m| comes to FAR it could be
+// more: the difference s - m is taken first then, which is exact where it matters.
 constexpr float FAR = 4194304.0f;
+__device__ __forceinline__ bool is_far(float m, float c2) { return !(fabsf(m * c2) < FAR); }           // (LOWEST is: c2 is 1e-30 or more)
+__device__ __forceinline__ float reference(float m, float c2) { return __builtin_fmaf(-m, c2, SHIFT); }
+// The exponent of the weight of score s under the maximum m is fma(s - less, c2, plus).
+struct Exponent {
+    float less, plus, c2;
+    __device__ __forceinline__ Exponent(float m, float c2_) : less(is_far(m, c2_) ? m : 0.0f), plus(is_far(m, c2_) ? SHIFT : reference(m, c2_)), c2(c2_) {}
+    __device__ __forceinline__ float operator()(float s) const { return __builtin_fmaf(s - less, c2, plus); }
+};
+// what takes sums of such weights to weights relative to 2^(c2 m) itself, but for the 2^SHIFT that all have: parts of a row meet there
+__device__ __forceinline__ float own_factor(float m, float c2) { return __builtin_amdgcn_exp2f(SHIFT - Exponent(m, c2)(m)); }
 
 // The granules that the rows r0 .. of a block see, and the parts that workgroups take of them, `chunk` each.
 struct Range { uint32_t first, count, parts, chunk; };

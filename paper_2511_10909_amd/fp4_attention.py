@@ -60,26 +60,36 @@ class Fp4Cache:
         free pages do not suffice."""
         if tokens < 0:
             raise ValueError("a sequence cannot be extended by %d tokens" % tokens)
-        if tokens == 0:
-            return
-        held, length = self._pages[sequence], self._lengths[sequence]
-        fresh = -(-(length + tokens) // self.page_tokens) - len(held)
-        shared = length % self.page_tokens and self._users[held[-1]] > 1
-        if max(fresh, 0) + bool(shared) > len(self._free):
-            raise ValueError("%d pages are asked for, %d are free" % (max(fresh, 0) + bool(shared), len(self._free)))
-        if shared:
-            page = self._free[-1]
-            self._copy([(held[-1], page)])
-            self._free.pop()
-            self._users[held[-1]] -= 1
-            self._users[page] = 1
-            held[-1] = page
-            self.generation += 1
-        for _ in range(fresh):
-            page = self._free.pop()
-            self._users[page] = 1
-            held.append(page)
-        self._lengths[sequence] = length + tokens
+        self._extend([sequence], [tokens])
+
+    def _extend(self, sequences, counts):
+        """All of the sequences or none: the pages are counted first, all copies are one call, and the bookkeeping follows it."""
+        taken, left, moves, steps = 0, {}, [], []                       # left: users that a page has lost to the copies so far
+        for s, n in zip(sequences, counts):
+            held, length = self._pages[s], self._lengths[s]
+            fresh = max(0, -(-(length + n) // self.page_tokens) - len(held))
+            # (the last of those who share a page keeps it)
+            shared = bool(n and length % self.page_tokens) and self._users[held[-1]] - left.get(held[-1], 0) > 1
+            if shared:
+                left[held[-1]] = left.get(held[-1], 0) + 1
+                if taken < len(self._free):
+                    moves.append((held[-1], self._free[-1 - taken]))
+            taken += shared + fresh
+            steps.append((s, n, shared, fresh))
+        if taken > len(self._free):
+            raise ValueError("%d pages are asked for, %d are free" % (taken, len(self._free)))
+        self._copy(moves)
+        for s, n, shared, fresh in steps:
+            held = self._pages[s]
+            if shared:
+                self._users[held[-1]] -= 1
+                held[-1] = self._free.pop()
+                self._users[held[-1]] = 1
+            for _ in range(fresh):
+                held.append(self._free.pop())
+                self._users[held[-1]] = 1
+            self._lengths[s] += n
+        self.generation += bool(moves)
 
     def fork(self, sequence):
         """A sequence with the same tokens, in the same pages.  Batches made before it are not for any further call: they would write into pages that are shared now."""
@@ -116,19 +126,11 @@ class Fp4Cache:
         return used
 
     def batch(self, sequences, tokens):
-        """Room for tokens[i] (or `tokens`) more tokens of sequences[i], and a Batch of them."""
+        """Room for tokens[i] (or `tokens`) more tokens of sequences[i], and a Batch of them.  Nothing changes if the free pages do not suffice or a page's copy fails."""
         counts = [tokens] * len(sequences) if isinstance(tokens, int) else list(tokens)
         if len(counts) != len(sequences) or len(set(sequences)) != len(sequences) or min(counts, default=0) < 0:
             raise ValueError("a batch has different sequences, and as many tokens of each as they are")
-        # (all or nothing: what extend would take of each, copies of shared pages included; a page that only these share may be counted once too often)
-        wanted = 0
-        for s, n in zip(sequences, counts):
-            held, length = self._pages[s], self._lengths[s]
-            wanted += max(0, -(-(length + n) // self.page_tokens) - len(held)) + bool(n and length % self.page_tokens and self._users[held[-1]] > 1)
-        if wanted > len(self._free):
-            raise ValueError("%d pages are asked for, %d are free" % (wanted, len(self._free)))
-        for s, n in zip(sequences, counts):
-            self.extend(s, n)
+        self._extend(sequences, counts)
         return Batch(self, list(sequences), counts)
 
 

@@ -136,13 +136,16 @@ class Fp4Cache:
 
 class Batch:
     """What the operators read of a call: page tables, lengths and first rows on the device.  A captured graph may count `lengths` on by itself, where the room for its
-    replays was taken beforehand (Fp4Cache.extend); a replay is not checked: fork, free and compact wait until it is done, and it is captured anew after them."""
+    replays was taken beforehand (Fp4Cache.extend); one whose tokens lie in shared pages is for reading alone; a replay is not checked: fork, free and compact wait until it is done, and it is captured anew after them."""
 
     def __init__(self, cache, sequences, counts):
         self.cache, self.sequences, self.generation = cache, sequences, cache.generation
         self.tokens, self.max_tokens = sum(counts), max(counts, default=0)
         lengths = [cache.length(s) for s in sequences]
         self.max_length = max(lengths, default=0)
+        # whether some of the call's tokens lie in pages that other sequences have as well (a batch that Fp4Cache.batch makes has none)
+        self.shared = any(cache._users[p] > 1 for s, n, length in zip(sequences, counts, lengths) if n
+                          for p in cache.pages_of(s)[max(length - n, 0) // cache.page_tokens:])
         columns = max([len(cache.pages_of(s)) for s in sequences] + [1])
         rows = [list(cache.pages_of(s)) + [-1] * (columns - len(cache.pages_of(s))) for s in sequences]
         first = [0]
@@ -195,6 +198,8 @@ class Fp4Attention:
         d, kv, tokens = cache.dim, cache.kv_heads, batch.tokens
         if batch.generation != cache.generation:
             raise ValueError("the batch is older than the last change of the cache's pages")
+        if batch.shared:
+            raise ValueError("the batch's tokens lie in pages that another sequence shares: Fp4Cache.batch and extend make room in pages of their own")
         _is_current(cache.device)
         if not 0 <= layer < cache.layers:
             raise ValueError("layer %d of a cache of %d" % (layer, cache.layers))

@@ -1,4 +1,4 @@
-"""Batches over shared pages (no GPU): one call copies all of them, and a batch that cannot be had changes nothing."""
+"""Batches over shared pages (no GPU): one call copies all of them, a batch that cannot be had changes nothing, and shared pages are not written."""
 import pytest
 import torch
 
@@ -96,3 +96,23 @@ def test_a_batch_without_room_changes_nothing(copies):
     with pytest.raises(KeyError):
         cache.batch([a, 99], 1)
     assert same(state(cache), before) and not calls
+
+
+def test_tokens_in_shared_pages_are_not_written(copies):
+    """A batch made of a sequence as it is, after a fork: its tokens are the other sequence's as well."""
+    cache = fa.Fp4Cache(1, 6, 1, 64, 32, device="cpu")
+    a, b = cache.new(), cache.new()
+    cache.extend(a, 40)
+    cache.extend(b, 64)
+    for s in (a, b):
+        assert not fa.Batch(cache, [s], [1]).shared
+    fork = cache.fork(a)
+    x, out = torch.zeros((9, 3 * 64), dtype=torch.bfloat16), torch.zeros((9, 64), dtype=torch.bfloat16)
+    for s, n in ((a, 1), (fork, 9)):
+        batch = fa.Batch(cache, [b, s], [0, n])
+        assert batch.shared
+        with pytest.raises(ValueError, match="shares"):
+            fa.Fp4Attention(1)(x, batch, 0, out)
+    assert not fa.Batch(cache, [a, b], [0, 64]).shared and not cache.batch([a, b], [1, 1]).shared
+    # a copy of its own for the last page, the first is shared still
+    assert not fa.Batch(cache, [a], [9]).shared and fa.Batch(cache, [a], [10]).shared

@@ -435,6 +435,8 @@ def cache_copy_pages(memory, moves, pages, page_bytes, layers=1, layer_bytes=0, 
     """Copies pages within each of `layers` caches; moves: pairs (from, to), a contiguous int32 tensor on the host."""
     if moves.dtype != torch.int32 or moves.device.type != "cpu" or not moves.is_contiguous() or moves.numel() % 2:
         raise ValueError("moves are pairs of 32-bit integers on the host, contiguous")
+    if isinstance(memory, torch.Tensor) and not memory.is_cuda:
+        raise ValueError("pages are copied in a GPU's memory, not on %s" % memory.device)
     _check(_lib.mmaemu_cache_copy_pages(_address(memory), moves.data_ptr(), moves.numel() // 2, pages, page_bytes, layers, layer_bytes, _stream(stream) or 0))
 
 

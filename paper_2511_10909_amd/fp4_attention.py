@@ -200,6 +200,8 @@ class Fp4Attention:
             raise ValueError("the batch is older than the last change of the cache's pages")
         if batch.shared:
             raise ValueError("the batch's tokens lie in pages that another sequence shares: Fp4Cache.batch and extend make room in pages of their own")
+        if cache.device.type != "cuda":
+            raise ValueError("attention runs on a GPU, the cache is on %s" % cache.device)
         _is_current(cache.device)
         if not 0 <= layer < cache.layers:
             raise ValueError("layer %d of a cache of %d" % (layer, cache.layers))

@@ -116,3 +116,21 @@ def test_tokens_in_shared_pages_are_not_written(copies):
     assert not fa.Batch(cache, [a, b], [0, 64]).shared and not cache.batch([a, b], [1, 1]).shared
     # a copy of its own for the last page, the first is shared still
     assert not fa.Batch(cache, [a], [9]).shared and fa.Batch(cache, [a], [10]).shared
+
+
+def test_a_cache_in_the_hosts_memory_is_not_for_the_gpu(monkeypatch):
+    """Its bookkeeping works; no kernel is given its addresses."""
+    def reached(*a, **kw):
+        raise AssertionError("a kernel's arguments were made")
+    for name in ("cache_append_fp4", "attention_fp4", "attention_fp4_workspace"):
+        monkeypatch.setattr(mm, name, reached)
+    monkeypatch.setattr(mm._lib, "mmaemu_cache_copy_pages", reached)
+    cache = fa.Fp4Cache(1, 4, 1, 64, 32, device="cpu")
+    a = cache.new()
+    batch = cache.batch([a], 3)
+    with pytest.raises(ValueError, match="GPU"):
+        fa.Fp4Attention(1)(torch.zeros((3, 3 * 64), dtype=torch.bfloat16), batch, 0, torch.zeros((3, 64), dtype=torch.bfloat16))
+    b = cache.fork(a)
+    with pytest.raises(ValueError, match="GPU"):
+        cache.extend(b, 1)
+    assert cache.pages_of(a) == cache.pages_of(b) and cache.free_pages() == 3

@@ -686,9 +686,9 @@ mmaemu_status mmaemu_cache_append_fp4(const mmaemu_cache_append_fp4_args *args);
  *   out[r][h] = sum over t of p_t v_t,  p = softmax over t of scale * (q[r][h] . k_t),  k and v of head h / (heads / kv_heads),
  * over the tokens t <= position of row r, and > position - window where window is not 0.  A row that sees no token gives zeros.  Tokens that a row does not
  * see have no part in it, whatever they hold.
- * Scores, maxima and sums are binary32; equal scores of a row have equal weights, whatever their size; the weights p, relative to a maximum that may lie 2^11 below the largest, are rounded to FP16 (nearest even) for the
- * second product: those below 2^-18 of the row's largest are off by up to 2^-29 of it.  A score that leaves binary32 is an infinity: tokens of minus infinity
- * weigh nothing, a row with one of plus infinity is NaN.
+ * Products q . k, maxima and sums are binary32; equal products of a row have equal weights, whatever their size; the weights p, relative to a maximum that may lie 2^11 below the
+ * largest, are rounded to FP16 (nearest even) for the second product: those below 2^-18 of the row's largest are off by up to 2^-29 of it.  A product that leaves binary32 (before the
+ * scale) is an infinity: tokens of minus infinity weigh nothing, a row that sees no others gives zeros, and a row with one of plus infinity is NaN.
  * max_length: the host's bound for lengths; it decides, with the other sizes, over how many workgroups a row's tokens are split, and nothing
  * else (longer sequences are computed all the same).  workspace: device memory of mmaemu_attention_fp4_workspace bytes, 16-byte aligned, for one call at a
  * time: calls that share it have to follow one another, those in graphs too.  NULL where that is 0.  One launch, or two where rows are split.  Results do
@@ -710,6 +710,10 @@ typedef struct {
 mmaemu_status mmaemu_attention_fp4(const mmaemu_attention_fp4_args *args);
 /* Bytes of workspace for these arguments (pointers, strides and scale are not looked at); decided on the host, no GPU needed. */
 mmaemu_status mmaemu_attention_fp4_workspace(const mmaemu_attention_fp4_args *args, uint64_t *bytes);
+/* What a call with these arguments is computed by, as text that the calling thread's next such query overwrites: "tokens over W wavefronts, ..." (a workgroup has all rows of a KV head) or
+ * "rows over W wavefronts, ...", the tiles of 16 rows that a wavefront has, the most parts of a row, and whether the longest sequences come first; "none" where there is nothing to do.  Decided on
+ * the host, no GPU needed; for tests and reports. */
+mmaemu_status mmaemu_attention_fp4_kernel(const mmaemu_attention_fp4_args *args, const char **name);
 
 /*
  * Copies pages within each of `layers` caches that lie layer_bytes apart (0: pages * page_bytes) from `memory` on: for each of `count` moves (HOST array of

@@ -150,6 +150,7 @@ _lib.mmaemu_matmul_fp4_packed.argtypes = [ctypes.c_char_p]
 _lib.mmaemu_cache_append_fp4.argtypes = [ctypes.c_char_p]
 _lib.mmaemu_attention_fp4.argtypes = [ctypes.c_char_p]
 _lib.mmaemu_attention_fp4_workspace.argtypes = [ctypes.c_char_p, ctypes.POINTER(_u64)]
+_lib.mmaemu_attention_fp4_kernel.argtypes = [ctypes.c_char_p, ctypes.POINTER(ctypes.c_char_p)]
 _lib.mmaemu_cache_copy_pages.argtypes = [_vp, _vp, _u64, _u64, _u64, _u64, _u64, _vp]
 _lib.mmaemu_matmul_fp4_kernel.argtypes = [_u32, _u32, _u32, ctypes.c_int, _u32, ctypes.POINTER(ctypes.c_char_p)]
 
@@ -405,13 +406,25 @@ def cache_append_fp4(q, k, v, q_out, cache, table, lengths, begins, type, *, dim
         _check(status)
 
 
+def _attention_sizes(type, *, dim, heads, kv_heads, page_tokens, pages, sequences, table_stride, tokens, max_tokens, max_length, window=0):
+    return _attention_pack(_ATTENTION_ARGS.size, type, dim, heads, kv_heads, page_tokens, sequences, max_tokens, max_length, window, 0, 0, 0, 0, 0, 0, 0, tokens, pages,
+                           table_stride, 0, 0, 0, 1.0, 0)
+
+
 def attention_fp4_workspace(type, *, dim, heads, kv_heads, page_tokens, pages, sequences, table_stride, tokens, max_tokens, max_length, window=0):
     """Bytes of workspace that attention_fp4 takes for these sizes."""
     size = _u64()
-    _check(_lib.mmaemu_attention_fp4_workspace(_ATTENTION_ARGS.pack(
-        _ATTENTION_ARGS.size, type, dim, heads, kv_heads, page_tokens, sequences, max_tokens, max_length, window, 0, 0, 0, 0, 0, 0, 0, tokens, pages, table_stride,
-        0, 0, 0, 1.0, 0), ctypes.byref(size)))
+    _check(_lib.mmaemu_attention_fp4_workspace(_attention_sizes(
+        type, dim=dim, heads=heads, kv_heads=kv_heads, page_tokens=page_tokens, pages=pages, sequences=sequences, table_stride=table_stride, tokens=tokens,
+        max_tokens=max_tokens, max_length=max_length, window=window), ctypes.byref(size)))
     return size.value
+
+
+def attention_fp4_kernel(type, **sizes):
+    """What attention_fp4 computes these sizes by; the arguments of attention_fp4_workspace."""
+    name = ctypes.c_char_p()
+    _check(_lib.mmaemu_attention_fp4_kernel(_attention_sizes(type, **sizes), ctypes.byref(name)))
+    return name.value.decode()
 
 
 def attention_fp4(q, out, cache, table, lengths, begins, workspace, type, *, dim, heads, kv_heads, page_tokens, pages, sequences, table_stride, tokens, max_tokens,

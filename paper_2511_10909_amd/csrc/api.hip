@@ -1084,6 +1084,18 @@ mmaemu_status mmaemu_attention_fp4_workspace(const mmaemu_attention_fp4_args *ar
     return MMAEMU_OK;
 }
 
+mmaemu_status mmaemu_attention_fp4_kernel(const mmaemu_attention_fp4_args *args, const char **name)
+{
+    static thread_local char text[96];
+    if (!is_args(args, sizeof(*args), "attention_fp4_kernel")) return MMAEMU_ERR_INVALID_ARG;
+    if (!name) { set_error("attention_fp4_kernel: NULL pointer"); return MMAEMU_ERR_INVALID_ARG; }
+    const mmaemu_status st = check_attention(*args);
+    if (st != MMAEMU_OK) return st;
+    attention_fp4_name(*args, text, sizeof(text));
+    *name = text;
+    return MMAEMU_OK;
+}
+
 mmaemu_status mmaemu_attention_fp4(const mmaemu_attention_fp4_args *args)
 {
     const char *what = "attention_fp4";

@@ -10,6 +10,8 @@
 // instructions hold for ten cycles, exponentials for eight and other vector instructions for four: 8192 tokens x 32 heads 541 us, 1.0 PFLOP/s of the products that are needed.
 #include "attention_fp4.hpp"
 
+#include <cstdio>
+
 namespace mmaemu {
 
 __device__ __forceinline__ float other_rows_max(float x)               // over lanes l, l + 16, l + 32, l + 48
@@ -482,6 +484,16 @@ static Plan plan_of(const mmaemu_attention_fp4_args &a)
     p.chunk = (uint32_t)((granules + p.splits - 1) / p.splits);
     if (p.chunk < 1) p.chunk = 1;
     return p;
+}
+
+void attention_fp4_name(const mmaemu_attention_fp4_args &a, char *text, size_t size)
+{
+    if (!a.sequences || !a.tokens || !a.max_tokens) {
+        snprintf(text, size, "none");
+        return;
+    }
+    const Plan p = plan_of(a);
+    snprintf(text, size, "%s over %u wavefronts, tiles %u, parts %u%s", p.row_waves > 1 ? "rows" : "tokens", p.waves, p.nr, p.splits, p.ordered ? ", longest first" : "");
 }
 
 uint64_t attention_fp4_workspace(const mmaemu_attention_fp4_args &a)

@@ -52,6 +52,7 @@ template <int D> __device__ __forceinline__ uint8_t *granule_at(const CacheArgs 
 mmaemu_status launch_cache_append(const mmaemu_cache_append_fp4_args &a, const CacheArgs &c, hipStream_t s);
 mmaemu_status launch_attention_fp4(const mmaemu_attention_fp4_args &a, const CacheArgs &c, hipStream_t s);
 uint64_t attention_fp4_workspace(const mmaemu_attention_fp4_args &a);
+void attention_fp4_name(const mmaemu_attention_fp4_args &a, char *text, size_t size);
 mmaemu_status launch_cache_copy(void *memory, const int32_t *moves, uint64_t count, uint64_t page_bytes, uint64_t layers, uint64_t layer_bytes, hipStream_t s);
 
 } // namespace mmaemu

@@ -708,7 +708,9 @@ typedef struct {
     void *hip_stream;
 } mmaemu_attention_fp4_args;
 mmaemu_status mmaemu_attention_fp4(const mmaemu_attention_fp4_args *args);
-/* Bytes of workspace for these arguments (pointers, strides and scale are not looked at); decided on the host, no GPU needed. */
+/* Bytes of workspace for these arguments (pointers, strides and scale are not looked at); decided on the host, no GPU needed.  A smaller call may need more: few rows, short
+ * sequences beside long ones or a window ask for more parts, and many sequences for none.  A program that keeps one workspace asks for each call that it makes, window included, or takes
+ * 268800 * (dim + 2) * 4 bytes (140 MB for heads of 128), which no call takes more than whose tokens are sequences * max_tokens at most. */
 mmaemu_status mmaemu_attention_fp4_workspace(const mmaemu_attention_fp4_args *args, uint64_t *bytes);
 /* What a call with these arguments is computed by, as text that the calling thread's next such query overwrites: "tokens over W wavefronts, ..." (a workgroup has all rows of a KV head) or
  * "rows over W wavefronts, ...", the tiles of 16 rows that a wavefront has, the most parts of a row, and whether the longest sequences come first; "none" where there is nothing to do.  Decided on
@@ -718,7 +720,7 @@ mmaemu_status mmaemu_attention_fp4_kernel(const mmaemu_attention_fp4_args *args,
 /*
  * Copies pages within each of `layers` caches that lie layer_bytes apart (0: pages * page_bytes) from `memory` on: for each of `count` moves (HOST array of
  * pairs: from, to) page `to` becomes page `from`.  All moves happen at once: no page may be the target of two moves, or the target of one and the source
- * of another; one page may be the source of several (a fork).  A page moved onto itself is left alone.  The moves are taken when the call is made, also
+ * of another; one page may be the source of several (a fork).  A page onto itself is no move.  The moves are taken when the call is made, also
  * into a captured graph.  page_bytes: a multiple of 16 (any cache's pages are).  count = 0 or layers = 0 is a no-op.
  * Errors: SHAPE (pages 0 or above 2^30, page_bytes 0, no multiple of 16 or above 2^32, layer_bytes below a layer's pages or no multiple of 16, layers above 65535,
  *         a layer above 2^46 bytes), INVALID_ARG (NULL or misaligned pointers, a page outside 0 .. pages - 1, targets as above), NOMEM (host memory for the checks).

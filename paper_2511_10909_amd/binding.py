@@ -412,7 +412,7 @@ def _attention_sizes(type, *, dim, heads, kv_heads, page_tokens, pages, sequence
 
 
 def attention_fp4_workspace(type, *, dim, heads, kv_heads, page_tokens, pages, sequences, table_stride, tokens, max_tokens, max_length, window=0):
-    """Bytes of workspace that attention_fp4 takes for these sizes."""
+    """Bytes of workspace that attention_fp4 takes for these sizes, which a smaller call may exceed: 268800 (dim + 2) 4 suffice for all with tokens <= sequences * max_tokens."""
     size = _u64()
     _check(_lib.mmaemu_attention_fp4_workspace(_attention_sizes(
         type, dim=dim, heads=heads, kv_heads=kv_heads, page_tokens=page_tokens, pages=pages, sequences=sequences, table_stride=table_stride, tokens=tokens,

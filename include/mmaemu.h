@@ -723,7 +723,7 @@ mmaemu_status mmaemu_attention_fp4_kernel(const mmaemu_attention_fp4_args *args,
  * of another; one page may be the source of several (a fork).  A page onto itself is no move.  The moves are taken when the call is made, also
  * into a captured graph.  page_bytes: a multiple of 16 (any cache's pages are).  count = 0 or layers = 0 is a no-op.
  * Errors: SHAPE (pages 0 or above 2^30, page_bytes 0, no multiple of 16 or above 2^32, layer_bytes below a layer's pages or no multiple of 16, layers above 65535,
- *         a layer above 2^46 bytes), INVALID_ARG (NULL or misaligned pointers, a page outside 0 .. pages - 1, targets as above), NOMEM (host memory for the checks).
+ *         a layer above 2^46 bytes, count above 2^32), INVALID_ARG (NULL or misaligned pointers, a page outside 0 .. pages - 1, targets as above), NOMEM (host memory for the checks).
  */
 mmaemu_status mmaemu_cache_copy_pages(void *memory, const int32_t *moves, uint64_t count, uint64_t pages, uint64_t page_bytes,
                                       uint64_t layers, uint64_t layer_bytes, void *hip_stream);

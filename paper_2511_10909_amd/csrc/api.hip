@@ -1122,8 +1122,8 @@ mmaemu_status mmaemu_cache_copy_pages(void *memory, const int32_t *moves, uint64
                                       void *hip_stream)
 {
     const char *what = "cache_copy_pages";
-    if (pages == 0 || pages > (1ull << 30) || page_bytes == 0 || page_bytes % 16 || page_bytes > (1ull << 32) || layers > 65535) {
-        set_error("%s: pages 1 .. 2^30, page_bytes a multiple of 16 up to 2^32, layers up to 65535", what);
+    if (pages == 0 || pages > (1ull << 30) || page_bytes == 0 || page_bytes % 16 || page_bytes > (1ull << 32) || layers > 65535 || count > (1ull << 32)) {
+        set_error("%s: pages 1 .. 2^30, page_bytes a multiple of 16 up to 2^32, layers up to 65535, count up to 2^32", what);
         return MMAEMU_ERR_SHAPE;
     }
     if (layer_bytes == 0) layer_bytes = pages * page_bytes;

@@ -689,6 +689,8 @@ mmaemu_status mmaemu_cache_append_fp4(const mmaemu_cache_append_fp4_args *args);
  * Products q . k, maxima and sums are binary32; equal products of a row have equal weights, whatever their size; the weights p, relative to a maximum that may lie 2^11 below the
  * largest, are rounded to FP16 (nearest even) for the second product: those below 2^-18 of the row's largest are off by up to 2^-29 of it.  A product that leaves binary32 (before the
  * scale) is an infinity: tokens of minus infinity weigh nothing, a row that sees no others gives zeros, and a row with one of plus infinity is NaN.
+ * One choice of rows and tokens a wavefront holds for the whole call, by max_tokens: up to 64 rows of a KV head (max_tokens * heads / kv_heads) have workgroups that share a sequence's tokens.
+ * Single tokens over long sequences are several times slower in one call with a chunk of more rows than in a call of their own.
  * max_length: the host's bound for lengths; it decides, with the other sizes, over how many workgroups a row's tokens are split, and nothing
  * else (longer sequences are computed all the same).  workspace: device memory of mmaemu_attention_fp4_workspace bytes, 16-byte aligned, for one call at a
  * time: calls that share it have to follow one another, those in graphs too.  NULL where that is 0.  One launch, or two where rows are split.  Results do

@@ -6,8 +6,8 @@
 // Both products are 16 x 16 x 32 instructions on operands that lie in the cache as the lanes take them (cache_fp4.hpp), brought to 16 bits, which is
 // exact: K to the queries' type, V to FP16.  The scores' registers are the second product's operand as they are, rounded to FP16.
 //
-// Few rows are bound by memory: 64 sequences of up to 16384 tokens, 64 heads over 8 of 128, 147 us, 4.9 TB/s.  Prompts are bound by the SIMDs' issue port, which matrix
-// instructions hold for ten cycles, exponentials for eight and other vector instructions for four: 8192 tokens x 32 heads 541 us, 1.0 PFLOP/s of the products that are needed.
+// Few rows are bound by memory: 64 sequences of up to 16384 tokens, 64 heads over 8 of 128, 148 us, 4.9 TB/s.  Prompts are bound by the SIMDs' issue port, which matrix
+// instructions hold for ten cycles, exponentials for eight and other vector instructions for four: 8192 tokens x 32 heads 540 us, 1.0 PFLOP/s of the products that are needed.
 #include "attention_fp4.hpp"
 
 #include <cstdio>
@@ -77,8 +77,8 @@ __device__ __forceinline__ uint32_t by_length(const CacheArgs &c, uint32_t k)
 }
 
 // Rows of NR x 16 x ROW_WAVES, tokens split over the other wavefronts.  Where the tiles of rows are many, the queries wait in LDS.  As many wavefronts a SIMD as registers
-// allow without scratch memory in the loop: two tiles of heads of 128 at three 134 us, at two 108 (3000 tokens x 32 heads); three tiles of heads of 64 at two 386 us,
-// at three, with five words of scratch, 350 (8192 tokens x 32 heads).
+// allow without scratch memory in the loop: two tiles of heads of 128 at three 134 us, at two 105 (3000 tokens x 32 heads); three tiles of heads of 64 at two 386 us,
+// at three 340 (8192 tokens x 32 heads).
 template <int T, int D, int NR, int ROW_WAVES, int WAVES> __global__ void __launch_bounds__(64 * WAVES, NR == 1 || (NR == 2 && D == 64) ? 4 : D == 64 ? 3 : 2) attention_kernel(const AttentionArgs a)
 {
     constexpr uint32_t TOKEN_WAVES = WAVES / ROW_WAVES, J = D / 32, DT = D / 16;
